@@ -304,11 +304,11 @@ def _plain_append(s):
     mine = torch.ldexp(kv, (1 - torch.frexp(scales[ids])[1]).double()[..., None].to(torch.int32))
     raw[ids, :, :, slot % page] = _codes(mine).view(torch.uint8)
     held = raw[tid][:, :, 0].view(torch.float8_e4m3fn).float()
-    counts = (torch.arange(page, device=DEV) < after[:, None])[:, None, :, None] & ~torch.isnan(held)
+    counts = (torch.arange(page, device=DEV) < after[:, None])[:, None, :, None]
+    held = torch.where(torch.isnan(held), torch.zeros_like(held), held)
     lo = torch.where(counts, held, torch.full_like(held, float("inf"))).amin(2)
     hi = torch.where(counts, held, torch.full_like(held, float("-inf"))).amax(2)
-    none = ~counts.any(2)
-    both = torch.stack([torch.where(none, torch.zeros_like(lo), lo), torch.where(none, torch.zeros_like(hi), hi)], 2)
+    both = torch.stack([lo, hi], 2)
     bounds.view(torch.uint8)[tid] = both.to(torch.float8_e4m3fn).view(torch.uint8)
     return {"codes": codes, "scales": scales, "bounds": bounds, "q": q}
 
