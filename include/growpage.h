@@ -457,6 +457,112 @@ int gp_attention_noalloc(const void* q, const void* k, const void* v, const int3
                          int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_len,
                          void* out, void* stream);
 
+/* ---- a cache of keys and values in 8 bits, in the caller's pages ------------------------------------ */
+
+/* (The paper has no counterpart of these calls; they stand beside the pool for requests that are kept whole, at half the
+ * pool's bytes per token, in pages that the caller's own scheduler hands out.)
+ *
+ * A gp_qcache describes one layer's cache: memory of the caller's, no handle, nothing kept between calls.  Keys and
+ * values are held as e4m3 numbers (4 exponent bits, bias 7, 3 mantissa bits, largest 448, no infinity) in the scale of
+ * their (page, KV head, keys | values), a power of two.  A scale is 2^e with the least e between -117 and 119 for which
+ * every finite element that was put into the page is at most 448 * 2^e in magnitude: it grows when a larger element is
+ * appended to a page that holds tokens already, and the codes there are then rounded to the new scale.  (Every held
+ * value is a bf16 number, and a code is off by half a step of its three mantissa bits at most; a power of two loses
+ * nothing in a floating-point code and makes the growth of a scale exact but for the smallest numbers.)  Elements that
+ * are infinite or not numbers are held as NaN and do not count for the scale; magnitudes above 448 * 2^119 as that.
+ * `bounds`, needed by gp_qcache_select only, has per (page, KV head) the smallest and the largest code of every
+ * channel of the keys held there (a NaN counts as 0).
+ * Pages may be shared between sequences as long as they are full. */
+typedef struct gp_qcache {
+  int32_t  n_kv_heads;
+  int32_t  head_dim;         /* d: 64 or 128                                                                           */
+  int32_t  page_size;        /* tokens per page: a power of two from 16 to 256                                         */
+  int32_t  device;           /* CUDA device of all the memory below and of the calls' streams                          */
+  int64_t  n_pages;
+  void*    codes;            /* device e4m3 [n_pages][n_kv_heads][2: keys, values][page_size][d], 16-byte aligned      */
+  float*   scales;           /* device fp32 [n_pages][n_kv_heads][2], 8-byte aligned                                   */
+  void*    bounds;           /* device e4m3 [n_pages][n_kv_heads][2: low, high][d], 16-byte aligned; NULL: none kept   */
+  int32_t* status;           /* device word that the kernels set bit 4 in when a page id they met is none of the
+                                cache's (the page is then skipped: nothing is written, its tokens count as absent);
+                                NULL: not told                                                                         */
+} gp_qcache;
+
+/* A packed batch: rows row_start[s] .. row_start[s + 1] - 1 of the batch's tensors belong to sequence s and are its
+ * newest tokens; seq_len[s] counts the tokens it holds with these rows.  Row i of r in a sequence of n tokens lies in
+ * slot n - r + i: page page_table[s][slot / page_size], place slot % page_size, and sees the slots up to its own.  A
+ * sequence may have no rows, a batch no sequences.  Rows behind row_start[n_seq] belong to nobody and are left as they are.  The three arrays
+ * are read on the device (they may change between replays of a captured graph); the host bounds below limit what
+ * is looked at: rows beyond max_rows of a sequence and tokens beyond max_len are not. */
+typedef struct gp_qbatch {
+  const int32_t* row_start;  /* device int32 [n_seq + 1], ascending                                                    */
+  const int32_t* seq_len;    /* device int32 [n_seq]                                                                   */
+  const int32_t* page_table; /* device int32 [n_seq][table_stride]                                                     */
+  int32_t n_seq, table_stride;
+  int32_t n_rows;            /* rows of the tensors                                                                    */
+  int32_t max_rows;          /* rows of one sequence at most                                                           */
+  int32_t max_len;           /* tokens of one sequence at most                                                         */
+  int32_t reserved;          /* keep 0                                                                                 */
+} gp_qbatch;
+
+/* element types */
+#define GP_TYPE_BF16 0
+#define GP_TYPE_F16  1
+#define GP_TYPE_F32  2       /* outputs of gp_qcache_attention only                                                    */
+
+/* New rows for gp_qcache_append.  Rows are [heads][d] with the given distance between rows, so that k, v and q may be
+ * slices of one projection's output. */
+typedef struct gp_qrows {
+  const void* k;             /* device [n_rows][n_kv_heads][d]                                                         */
+  const void* v;
+  const void* q;             /* device [n_rows][n_q_heads][d]; NULL: no queries                                        */
+  void*       q_out;         /* the queries normalised and rotated, same type; may be q itself (with q_out_stride = q_stride) */
+  int64_t k_stride, v_stride, q_stride, q_out_stride;   /* elements from row to row, multiples of 8                    */
+  const int32_t* positions;  /* device int32 [n_rows]: positions of the rotation; NULL: a row's slot                   */
+  const float* q_weight;     /* device fp32 [d]: x <- x / sqrt(mean(x^2) + eps) * weight per head; NULL: no normalisation */
+  const float* k_weight;
+  double  eps;
+  double  rope_theta;        /* base of the rotation (rotate-half pairing); 0: none                                    */
+  int32_t n_q_heads;
+  int32_t type;              /* GP_TYPE_BF16 or GP_TYPE_F16: k, v, q and q_out                                         */
+} gp_qrows;
+
+/* Puts the batch's rows into the cache: normalised (optional), rotated (optional), in e4m3, with the scales and, where
+ * the cache has them, the bounds of the pages they touch; the queries with them.  Keys are computed in fp64 (their
+ * largest magnitude decides the scale's exponent), queries in fp32, rounded once.  k, v, q, q_out 16-byte aligned;
+ * a page that receives rows must belong to one sequence of the batch only.  Sequences by themselves may have their
+ * rows appended again: the same codes result.  Asynchronous on `stream`, no workspace; can be captured. */
+int gp_qcache_append(const gp_qcache* cache, const gp_qbatch* batch, const gp_qrows* rows, void* stream);
+
+/* Attention of the batch's rows over the cache: out = softmax(q.k / sqrt(d)).v over the slots that a row sees, per
+ * query head, KV head g / G.  Single tokens, drafts and chunks of prompts alike.  q is in cache form (as
+ * gp_qcache_append leaves it), finite.
+ *   q, q_stride  device [n_rows][n_q_heads][d] of `type` (GP_TYPE_BF16, GP_TYPE_F16), elements from row to row (a
+ *                multiple of 8), 16-byte aligned
+ *   pages        NULL: all pages.  Else device int32 [n_rows][n_kv_heads][n_list]: the pages (places in the sequence's
+ *                page table) that each row and KV head looks at, each at most once, in any order, -1 for none; places
+ *                beyond the row's own page count as none
+ *   out          device [n_rows][n_q_heads][d] of `out_type` (any GP_TYPE_*), 16-byte aligned; zeros where a row sees nothing
+ *   work         device memory of at least gp_qcache_attention_bytes(...) bytes for the same arguments, 16-byte aligned (may
+ *                be NULL where that is 0).  Nothing in it has to be cleared or kept; calls that may overlap on the
+ *                GPU need work memory of their own
+ * n_q_heads / n_kv_heads is at most 8.  Asynchronous on `stream`; can be captured. */
+int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batch, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t type,
+                        const int32_t* pages, int32_t n_list, void* out, int32_t out_type, void* work, size_t work_bytes, void* stream);
+size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch, int32_t n_q_heads, int32_t n_list);
+
+/* Chooses the pages that a row's attention over a list looks at, per KV head.  A row sees the pages 0 .. m - 1 up to its
+ * own.  Where m <= keep it gets them all; else the `first` first, the `recent` last, and of the others those with
+ * the highest
+ *     score = 2^e * sum over channels c of ( high_c * sum_g max(q_gc, 0) + low_c * sum_g min(q_gc, 0) ),
+ * the sum over the group's query heads of the largest q.k that a key within the page's bounds can have; equal scores go
+ * to the lower page.  fp64 throughout (integers come out of it).  NaN scores count as lowest.
+ *   pages   device int32 [n_rows][n_kv_heads][keep]: ascending, -1 behind the last
+ * 1 <= recent, 0 <= first, first + recent <= keep.  q and work as for gp_qcache_attention (gp_qcache_select_bytes).  A page
+ * whose id is none of the cache's has the lowest score. */
+int gp_qcache_select(const gp_qcache* cache, const gp_qbatch* batch, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t type,
+                     int32_t keep, int32_t first, int32_t recent, int32_t* pages, void* work, size_t work_bytes, void* stream);
+size_t gp_qcache_select_bytes(const gp_qcache* cache, const gp_qbatch* batch);
+
 #ifdef __cplusplus
 }
 #endif

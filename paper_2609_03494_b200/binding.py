@@ -40,6 +40,35 @@ class gp_config(C.Structure):
     ]
 
 
+GP_TYPE_BF16, GP_TYPE_F16, GP_TYPE_F32 = 0, 1, 2
+
+
+class gp_qcache(C.Structure):
+    _fields_ = [
+        ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32), ("device", C.c_int32),
+        ("n_pages", C.c_int64),
+        ("codes", C.c_void_p), ("scales", C.c_void_p), ("bounds", C.c_void_p), ("status", C.c_void_p),
+    ]
+
+
+class gp_qbatch(C.Structure):
+    _fields_ = [
+        ("row_start", C.c_void_p), ("seq_len", C.c_void_p), ("page_table", C.c_void_p),
+        ("n_seq", C.c_int32), ("table_stride", C.c_int32), ("n_rows", C.c_int32), ("max_rows", C.c_int32),
+        ("max_len", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class gp_qrows(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("q", C.c_void_p), ("q_out", C.c_void_p),
+        ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_stride", C.c_int64), ("q_out_stride", C.c_int64),
+        ("positions", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+        ("eps", C.c_double), ("rope_theta", C.c_double),
+        ("n_q_heads", C.c_int32), ("type", C.c_int32),
+    ]
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -89,6 +118,12 @@ def lib() -> C.CDLL:
     L.gp_get_kernel_times.argtypes = [vp, vp, vp]
     L.gp_launch_count.argtypes = [vp]; L.gp_launch_count.restype = i64
     L.gp_attention_noalloc.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    sz, qc, qb = C.c_size_t, C.POINTER(gp_qcache), C.POINTER(gp_qbatch)
+    L.gp_qcache_append.argtypes = [qc, qb, C.POINTER(gp_qrows), vp]
+    L.gp_qcache_attention.argtypes = [qc, qb, vp, i64, i32, i32, vp, i32, vp, i32, vp, sz, vp]
+    L.gp_qcache_attention_bytes.argtypes = [qc, qb, i32, i32]; L.gp_qcache_attention_bytes.restype = sz
+    L.gp_qcache_select.argtypes = [qc, qb, vp, i64, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+    L.gp_qcache_select_bytes.argtypes = [qc, qb]; L.gp_qcache_select_bytes.restype = sz
     _lib = L
     return L
 
@@ -333,7 +368,31 @@ def gp_attention_noalloc(q_ptr: int, k_ptr: int, v_ptr: int, lens_ptr: int, n_re
                                       C.c_void_p(stream)), "gp_attention_noalloc")
 
 
-# ------------------------------------------------------------------------------- convenience holder
+def gp_qcache_append(cache: gp_qcache, batch: gp_qbatch, rows: gp_qrows, stream: int) -> None:
+    _check(lib().gp_qcache_append(C.byref(cache), C.byref(batch), C.byref(rows), stream), "gp_qcache_append")
+
+
+def gp_qcache_attention_bytes(cache: gp_qcache, batch: gp_qbatch, n_q_heads: int, n_list: int) -> int:
+    return int(lib().gp_qcache_attention_bytes(C.byref(cache), C.byref(batch), n_q_heads, n_list))
+
+
+def gp_qcache_attention(cache: gp_qcache, batch: gp_qbatch, q_ptr: int, q_stride: int, n_q_heads: int, type: int, pages_ptr: int, n_list: int,
+                        out_ptr: int, out_type: int, work_ptr: int, work_bytes: int, stream: int) -> None:
+    _check(lib().gp_qcache_attention(C.byref(cache), C.byref(batch), q_ptr, q_stride, n_q_heads, type, pages_ptr, n_list, out_ptr, out_type,
+                                     work_ptr, work_bytes, stream), "gp_qcache_attention")
+
+
+def gp_qcache_select_bytes(cache: gp_qcache, batch: gp_qbatch) -> int:
+    return int(lib().gp_qcache_select_bytes(C.byref(cache), C.byref(batch)))
+
+
+def gp_qcache_select(cache: gp_qcache, batch: gp_qbatch, q_ptr: int, q_stride: int, n_q_heads: int, type: int, keep: int, first: int,
+                     recent: int, pages_ptr: int, work_ptr: int, work_bytes: int, stream: int) -> None:
+    _check(lib().gp_qcache_select(C.byref(cache), C.byref(batch), q_ptr, q_stride, n_q_heads, type, keep, first, recent, pages_ptr, work_ptr,
+                                  work_bytes, stream), "gp_qcache_select")
+
+
+# ------------------------------------------------------------------------------- convenience holders
 class Pool:
     """Owns the torch blob and the handle of one pool, and marshals torch tensors into the calls above."""
 
@@ -412,6 +471,140 @@ class Pool:
             self.close()
         except Exception:
             pass
+
+
+class QBatch:
+    """A packed batch over an 8-bit cache (gp_qbatch): row_start int32 [n_seq + 1], seq_len int32 [n_seq] and page_table int32
+    [n_seq][stride] are torch CUDA tensors of the caller's, kept alive and read on the device whenever a call runs."""
+
+    def __init__(self, row_start, seq_len, page_table, n_rows: int, max_rows: int, max_len: int):
+        import torch
+        for name, t, dims in (("row_start", row_start, 1), ("seq_len", seq_len, 1), ("page_table", page_table, 2)):
+            if t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name}: a contiguous int32 CUDA tensor of {dims} dimension(s) is needed")
+        n_seq = seq_len.shape[0]
+        if row_start.shape[0] != n_seq + 1 or page_table.shape[0] != n_seq:
+            raise ValueError("row_start has one entry more than seq_len, page_table a row for each of its entries")
+        if not seq_len.device == row_start.device == page_table.device:
+            raise ValueError("row_start, seq_len and page_table lie on one device")
+        self.tensors = (row_start, seq_len, page_table)
+        self.device = seq_len.device
+        self.n_rows = n_rows
+        self.desc = gp_qbatch(row_start.data_ptr(), seq_len.data_ptr(), page_table.data_ptr(), n_seq, page_table.shape[1], n_rows, max_rows,
+                              max_len, 0)
+
+
+class QCache:
+    """One layer's 8-bit cache (gp_qcache) over torch CUDA tensors of the caller's: codes float8_e4m3fn [n_pages][n_kv_heads][2][page][d],
+    scales float32 [n_pages][n_kv_heads][2], bounds float8_e4m3fn [n_pages][n_kv_heads][2][d] or None, status int32 [1] or None.
+    Calls run on the current stream of the tensors' device; work memory and results come from torch's allocator."""
+
+    def __init__(self, codes, scales, bounds=None, status=None):
+        import torch
+        self.torch = torch
+        self._types = {torch.bfloat16: GP_TYPE_BF16, torch.float16: GP_TYPE_F16, torch.float32: GP_TYPE_F32}
+        if codes.dim() != 5 or codes.shape[2] != 2:
+            raise ValueError("codes: [n_pages][n_kv_heads][2][page_size][head_dim]")
+        n_pages, heads, _, page, d = codes.shape
+        for name, t, dtype, shape in (("codes", codes, torch.float8_e4m3fn, codes.shape), ("scales", scales, torch.float32, (n_pages, heads, 2)),
+                                      ("bounds", bounds, torch.float8_e4m3fn, (n_pages, heads, 2, d)), ("status", status, torch.int32, (1,))):
+            if t is None:
+                continue
+            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda or t.device != codes.device:
+                raise ValueError(f"{name}: a contiguous {dtype} CUDA tensor {tuple(shape)} on the cache's device is needed")
+        self.tensors = (codes, scales, bounds, status)
+        self.device = codes.device
+        self.n_kv_heads, self.head_dim, self.page_size = heads, d, page
+        self.desc = gp_qcache(heads, d, page, codes.device.index, n_pages, codes.data_ptr(), scales.data_ptr(),
+                              bounds.data_ptr() if bounds is not None else None, status.data_ptr() if status is not None else None)
+
+    @classmethod
+    def create(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 16, device: int = 0, bounds: bool = True) -> "QCache":
+        """A cache with memory of its own (zeros)."""
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("a CUDA device is required; there is no CPU fallback")
+        kw = dict(device=f"cuda:{device}")
+        f8 = lambda *shape: torch.zeros(shape, dtype=torch.uint8, **kw).view(torch.float8_e4m3fn)  # noqa: E731
+        return cls(f8(n_pages, n_kv_heads, 2, page_size, head_dim), torch.ones((n_pages, n_kv_heads, 2), dtype=torch.float32, **kw),
+                   f8(n_pages, n_kv_heads, 2, head_dim) if bounds else None, torch.zeros(1, dtype=torch.int32, **kw))
+
+    def stream(self) -> int:
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def _rows(self, name: str, t, batch: QBatch, heads: int, dtype=None) -> int:
+        """Checks a [n_rows][heads][head_dim] tensor whose rows may be apart; returns the distance between them."""
+        if t.dim() != 3 or t.shape[0] != batch.n_rows or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
+            raise ValueError(f"{name}: [n_rows][heads][head_dim] is needed")
+        if t.device != self.device or batch.device != self.device:
+            raise ValueError(f"{name}, batch and cache lie on one device")
+        if t.dtype not in self._types or t.dtype == self.torch.float32 or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"{name}: bfloat16 or float16 is needed, the same for all")
+        stride, head, elem = t.stride()
+        if elem != 1 or (head != self.head_dim and t.shape[1] > 1):
+            raise ValueError(f"{name}: the heads of a row lie one behind the other")
+        return max(stride, t.shape[1] * self.head_dim) if batch.n_rows <= 1 else stride
+
+    def append(self, batch: QBatch, k, v, q=None, q_out=None, positions=None, rope_theta: float = 0.0, q_weight=None, k_weight=None,
+               eps: float = 1e-6):
+        """Puts the batch's rows into the cache (gp_qcache_append); returns the normalised and rotated queries (q_out, a new tensor where
+        none is given), or None without q."""
+        torch = self.torch
+        rows = gp_qrows(k=k.data_ptr(), v=v.data_ptr(), k_stride=self._rows("k", k, batch, self.n_kv_heads),
+                        v_stride=self._rows("v", v, batch, self.n_kv_heads, k.dtype), eps=eps, rope_theta=rope_theta, type=self._types[k.dtype])
+        for name, t, dtype, n in (("positions", positions, torch.int32, batch.n_rows), ("q_weight", q_weight, torch.float32, self.head_dim),
+                                  ("k_weight", k_weight, torch.float32, self.head_dim)):
+            if t is not None:
+                if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} on the cache's device is needed")
+                setattr(rows, name, t.data_ptr())
+        if q is not None:
+            rows.q, rows.q_stride, rows.n_q_heads = q.data_ptr(), self._rows("q", q, batch, 0, k.dtype), q.shape[1]
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
+            rows.q_out, rows.q_out_stride = q_out.data_ptr(), self._rows("q_out", q_out, batch, q.shape[1], k.dtype)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        gp_qcache_append(self.desc, batch.desc, rows, self.stream())
+        return q_out
+
+    def attention(self, batch: QBatch, q, out=None, out_dtype=None, pages=None):
+        """Attention of the batch's rows (gp_qcache_attention): all pages, or pages int32 [n_rows][n_kv_heads][n_list]."""
+        torch = self.torch
+        stride = self._rows("q", q, batch, 0)
+        if out is None:
+            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
+        elif tuple(out.shape) != tuple(q.shape) or not out.is_contiguous() or out.device != self.device or (out_dtype or out.dtype) != out.dtype:
+            raise ValueError("out: a contiguous tensor of the queries' shape on the cache's device is needed")
+        if out.dtype not in self._types:
+            raise ValueError("out: bfloat16, float16 or float32 is needed")
+        n_list = 0
+        if pages is not None:
+            n_list = pages.shape[-1]
+            if pages.dtype != torch.int32 or tuple(pages.shape) != (batch.n_rows, self.n_kv_heads, n_list) or n_list < 1 or \
+                    not pages.is_contiguous() or pages.device != self.device:
+                raise ValueError("pages: a contiguous int32 tensor [n_rows][n_kv_heads][n_list] on the cache's device is needed")
+        need = gp_qcache_attention_bytes(self.desc, batch.desc, q.shape[1], n_list)
+        work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        gp_qcache_attention(self.desc, batch.desc, q.data_ptr(), stride, q.shape[1], self._types[q.dtype],
+                            pages.data_ptr() if n_list else None, n_list, out.data_ptr(), self._types[out.dtype],
+                            work.data_ptr() if need else None, need, self.stream())
+        return out
+
+    def select(self, batch: QBatch, q, keep: int, first: int = 1, recent: int = 1, pages=None):
+        """The pages a row looks at per KV head (gp_qcache_select): int32 [n_rows][n_kv_heads][keep], ascending, -1 behind the last."""
+        torch = self.torch
+        stride = self._rows("q", q, batch, 0)
+        shape = (batch.n_rows, self.n_kv_heads, keep)
+        if pages is None:
+            pages = torch.empty(shape, dtype=torch.int32, device=self.device)
+        elif pages.dtype != torch.int32 or tuple(pages.shape) != shape or not pages.is_contiguous() or pages.device != self.device:
+            raise ValueError(f"pages: a contiguous int32 tensor {shape} on the cache's device is needed")
+        need = gp_qcache_select_bytes(self.desc, batch.desc)
+        work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        gp_qcache_select(self.desc, batch.desc, q.data_ptr(), stride, q.shape[1], self._types[q.dtype], keep, first, recent, pages.data_ptr(),
+                         work.data_ptr() if need else None, need, self.stream())
+        return pages
 
 
 def make_config(n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_pages_per_req: int,

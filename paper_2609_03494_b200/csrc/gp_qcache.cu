@@ -1,0 +1,656 @@
+// gp_qcache_append and gp_qcache_select: what goes into the 8-bit cache, and which of its pages a row looks at.
+#include "gp_qcache.cuh"
+
+namespace {
+
+// ================================================================================================ append
+struct QcRows {                // gp_qrows
+  const unsigned short *k, *v, *q;
+  unsigned short* q_out;
+  long long k_stride, v_stride, q_stride, qo_stride;
+  const int* positions;
+  const float *qw, *kw;
+  double eps;
+  int Hq, f16, rope;
+};
+struct QcFreq { double over_pi[64]; };      // theta^(-2i/d) / pi: angles in units of pi
+
+constexpr int QA_THREADS = 256;
+constexpr int QA_WARPS = QA_THREADS / 32;
+
+// least e with amax <= 448 * 2^e = 0.875 * 2^(e + 9)
+__device__ __forceinline__ int qc_exponent(double amax) {
+  if (!(amax > 0.0)) return QC_E_MIN;
+  int x;
+  const double f = frexp(amax, &x);
+  return min(max(x - 9 + (f > 0.875 ? 1 : 0), QC_E_MIN), QC_E_MAX);
+}
+__device__ __forceinline__ int qc_scale_exponent(float s) {      // of a scale that is there; anything else is brought into the range
+  return min(max((int)((__float_as_uint(s) >> 23) & 255) - 127, QC_E_MIN), QC_E_MAX);
+}
+__device__ __forceinline__ float pow2f(int e) {                  // 2^e, 0 below the normal numbers
+  return e < -126 ? 0.f : __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// A team of TEAM warps takes one (page, KV head) at a time, keys first, then values: a row lies in D / 8 lanes (four elements of
+// its first half and four of its second, so that a lane has both elements of the pairs it rotates), a team takes TEAM * 256 / D rows in a
+// pass and keeps up to PASSES passes in registers until the largest magnitude of all of them is known.  The angles of the block's tokens
+// are computed once for all heads (TABLE), in fp64, as the keys are: their largest magnitude decides an integer, and against a definition
+// in 64 bits only 64 bits decide it alike.  Values need no arithmetic before their maximum.
+// Queries (the last blocks of the grid) decide nothing: fp32, with angles reduced in fp64.
+template <int D, int TEAM, int PASSES, bool TABLE>
+__global__ void __launch_bounds__(QA_THREADS)
+qc_append_kernel(const QcDev c, const QcRows r, const __grid_constant__ QcFreq freq, int places, int groups, int heads_per, int kv_blocks,
+                 int q_rows) {
+  constexpr int LPR = D / 8;                          // lanes per row
+  constexpr int RPW = 32 / LPR;                       // rows of a warp in a pass
+  constexpr int HALF = D / 2;
+  extern __shared__ uint8_t qa_smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane % LPR, sub = lane / LPR;
+  const bool f16 = r.f16 != 0;
+
+  if ((int)blockIdx.x >= kv_blocks) {                 // ---- queries: q_rows rows of the batch
+    __shared__ int s_pos[16], s_has[16];
+    float2* tab = reinterpret_cast<float2*>(qa_smem); // [q_rows][HALF] cos, sin
+    const int base = ((int)blockIdx.x - kv_blocks) * q_rows;
+    if (tid < 16) s_pos[tid] = s_has[tid] = 0;
+    __syncthreads();
+    for (int s = tid; s < c.n_seq; s += QA_THREADS) {
+      const QcSeq q = qc_seq(c, s);
+      for (int i = max(q.r0, base); i < min(q.r0 + q.rows, base + q_rows); ++i) {
+        const int slot = q.slot0 + i - q.r0;
+        if (slot >= 0 && slot < c.limit) { s_pos[i - base] = r.positions ? r.positions[i] : slot; s_has[i - base] = 1; }
+      }
+    }
+    __syncthreads();
+    if (r.rope) {
+      for (int i = tid; i < q_rows * HALF; i += QA_THREADS) {
+        const double a = s_pos[i / HALF] * freq.over_pi[i % HALF];
+        float sn, cs;
+        sincospif((float)(a - 2.0 * rint(0.5 * a)), &sn, &cs);
+        tab[i] = make_float2(cs, sn);
+      }
+      __syncthreads();
+    }
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = r.qw ? r.qw[lr * 4 + (e & 3) + (e >> 2) * HALF] : 1.f;
+    constexpr int PER = QA_THREADS / LPR, U = 4;      // rows (of one head) of the block in a pass; passes whose loads go out together
+    const int n = q_rows * r.Hq;
+    for (int i0 = warp * RPW + sub; i0 - sub < n; i0 += PER * U) {
+      uint2 raw[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * PER, t = i / r.Hq, h = i % r.Hq;
+        raw[u][0] = raw[u][1] = make_uint2(0, 0);
+        if (i < n && s_has[t]) {
+          const unsigned short* src = r.q + (size_t)(base + t) * r.q_stride + h * D + lr * 4;
+          raw[u][0] = *reinterpret_cast<const uint2*>(src);
+          raw[u][1] = *reinterpret_cast<const uint2*>(src + HALF);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * PER, t = min(i, n - 1) / r.Hq, h = i % r.Hq;
+        float x[8];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const float2 a = qc_elems(raw[u][hf].x, f16), b = qc_elems(raw[u][hf].y, f16);
+          x[hf * 4] = a.x; x[hf * 4 + 1] = a.y; x[hf * 4 + 2] = b.x; x[hf * 4 + 3] = b.y;
+        }
+        if (r.qw) {
+          float ss = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+#pragma unroll
+          for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+          const float inv = 1.f / sqrtf(ss * (1.f / D) + (float)r.eps);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= inv * w[e];
+        }
+        if (r.rope) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 cs = tab[t * HALF + lr * 4 + e];
+            const float a = x[e], b = x[e + 4];
+            x[e] = a * cs.x - b * cs.y;
+            x[e + 4] = b * cs.x + a * cs.y;
+          }
+        }
+        if (i < n && s_has[t]) {
+          unsigned short* dst = r.q_out + (size_t)(base + t) * r.qo_stride + h * D + lr * 4;
+          *reinterpret_cast<uint2*>(dst) = make_uint2(qc_pack(x[0], x[1], f16), qc_pack(x[2], x[3], f16));
+          *reinterpret_cast<uint2*>(dst + HALF) = make_uint2(qc_pack(x[4], x[5], f16), qc_pack(x[6], x[7], f16));
+        }
+      }
+    }
+    return;
+  }
+
+  // ---- keys and values: one page's new rows, heads_per heads
+  constexpr int TEAMS = QA_WARPS / TEAM;
+  __shared__ double s_max[QA_WARPS];
+  __shared__ uint32_t s_bnd[TEAM > 1 ? QA_WARPS : 1][2][TEAM > 1 ? HALF : 1];
+  double2* tab = reinterpret_cast<double2*>(qa_smem); // [new rows][HALF] cos, sin
+  const int team = warp / TEAM, tw = warp % TEAM;
+  int at = blockIdx.x;
+  const int grp = at % groups; at /= groups;
+  const int place = at % places, s = at / places;
+  const QcSeq q = qc_seq(c, s);
+  const int first = max(q.slot0, 0), end = min(q.slot0 + q.rows, c.limit);        // slots the batch fills
+  const int lp = (first >> c.page_log) + place;
+  const int a = max(first, lp << c.page_log), z = min(end, (lp + 1) << c.page_log);
+  if (a >= z) return;
+  const int nt = z - a, kept = a & (c.page - 1);      // new rows; rows the page holds already
+  const int row0 = q.r0 + a - q.slot0;                // batch row of the first new one
+  const int pid = qc_page(c, s, lp);
+  if (pid < 0) return;
+  auto team_sync = [&]() {
+    if (TEAM == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM * 32) : "memory");
+  };
+  auto angle = [&](int t, int i) {
+    const int p = r.positions ? r.positions[row0 + t] : a + t;
+    double2 cs;
+    sincospi(p * freq.over_pi[i], &cs.y, &cs.x);
+    return cs;
+  };
+  if (TABLE && r.rope) {
+    for (int i = tid; i < nt * HALF; i += QA_THREADS) tab[i] = angle(i / HALF, i % HALF);
+    __syncthreads();
+  }
+  const int h1 = min((grp + 1) * heads_per, c.Hkv);
+  for (int h = grp * heads_per + team; h < h1; h += TEAMS) {
+    const size_t unit = (size_t)pid * c.Hkv + h;
+    float2 old_scale = make_float2(1.f, 1.f);
+    if (kept) old_scale = *reinterpret_cast<const float2*>(c.scales + unit * 2);
+    uint2 kraw[PASSES][2], vraw[PASSES][2];
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      const int t = (u * TEAM + tw) * RPW + sub;
+      kraw[u][0] = kraw[u][1] = vraw[u][0] = vraw[u][1] = make_uint2(0, 0);
+      if (t < nt) {
+        const unsigned short* ks = r.k + (size_t)(row0 + t) * r.k_stride + h * D + lr * 4;
+        const unsigned short* vs = r.v + (size_t)(row0 + t) * r.v_stride + h * D + lr * 4;
+        kraw[u][0] = *reinterpret_cast<const uint2*>(ks);
+        kraw[u][1] = *reinterpret_cast<const uint2*>(ks + HALF);
+        vraw[u][0] = *reinterpret_cast<const uint2*>(vs);
+        vraw[u][1] = *reinterpret_cast<const uint2*>(vs + HALF);
+      }
+    }
+    float x[PASSES][8];
+    double kmax = 0.0;
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      const int t = (u * TEAM + tw) * RPW + sub;
+      double y[8];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const float2 e0 = qc_elems(kraw[u][hf].x, f16), e1 = qc_elems(kraw[u][hf].y, f16);
+        y[hf * 4] = e0.x; y[hf * 4 + 1] = e0.y; y[hf * 4 + 2] = e1.x; y[hf * 4 + 3] = e1.y;
+      }
+      if (r.kw) {
+        double ss = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const double inv = 1.0 / sqrt(ss * (1.0 / D) + r.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= inv * (double)r.kw[lr * 4 + (e & 3) + (e >> 2) * HALF];
+      }
+      if (r.rope && t < nt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double2 cs = TABLE ? tab[t * HALF + lr * 4 + e] : angle(t, lr * 4 + e);
+          const double p = y[e], m = y[e + 4];
+          y[e] = p * cs.x - m * cs.y;
+          y[e + 4] = m * cs.x + p * cs.y;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float f = (float)y[e];
+        if (fabs(y[e]) < INFINITY) {                  // (finite in 64 bits)
+          kmax = fmax(kmax, fabs(y[e]));
+          if (!(fabsf(f) < INFINITY)) f = copysignf(3.402823466e38f, f);
+        }
+        x[u][e] = f;
+      }
+    }
+    float vmax = 0.f;
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const float2 e0 = qc_elems(vraw[u][hf].x, f16), e1 = qc_elems(vraw[u][hf].y, f16);
+        for (float f : {e0.x, e0.y, e1.x, e1.y}) if (fabsf(f) < INFINITY) vmax = fmaxf(vmax, fabsf(f));
+      }
+    // the team's largest magnitudes
+    double vm = vmax;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      kmax = fmax(kmax, __shfl_xor_sync(0xffffffffu, kmax, o));
+      vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
+    }
+    vm = vmax;
+    if (TEAM > 1) {
+      if (lane == 0) s_max[warp] = kmax;
+      team_sync();
+#pragma unroll
+      for (int o = 0; o < TEAM; ++o) kmax = fmax(kmax, s_max[team * TEAM + o]);
+      team_sync();
+      if (lane == 0) s_max[warp] = vm;
+      team_sync();
+#pragma unroll
+      for (int o = 0; o < TEAM; ++o) vm = fmax(vm, s_max[team * TEAM + o]);
+      team_sync();
+    }
+    int ek = qc_exponent(kmax), ev = qc_exponent(vm);
+    const int ek0 = qc_scale_exponent(old_scale.x), ev0 = qc_scale_exponent(old_scale.y);
+    if (kept) { ek = max(ek, ek0); ev = max(ev, ev0); }
+    uint8_t* kdst = c.codes + unit * 2 * c.page * D;
+    uint8_t* vdst = kdst + (size_t)c.page * D;
+    if (kept && (ek != ek0 || ev != ev0)) {           // rows that are there already, rounded to the new scale
+      for (int i = tw * 32 + lane; i < 2 * kept * (D / 16); i += TEAM * 32) {
+        const bool isv = i >= kept * (D / 16);
+        const int by = isv ? ev0 - ev : ek0 - ek;
+        if (by == 0) continue;
+        uint4* p = reinterpret_cast<uint4*>(isv ? vdst : kdst) + (isv ? i - kept * (D / 16) : i);
+        uint4 w = *p;
+        const float m = pow2f(by);
+        for (uint32_t* e : {&w.x, &w.y, &w.z, &w.w}) {
+          const float2 lo = qc_half2(e4m3x2_to_f16x2(*e)), hi = qc_half2(e4m3x2_hi_to_f16x2(*e));
+          *e = qc_codes(lo.x * m, lo.y * m, hi.x * m, hi.y * m);
+        }
+        *p = w;
+      }
+    }
+    // codes of the new rows; bounds from the codes, as pairs of fp16
+    const uint32_t PINF2 = 0x7c007c00u, NINF2 = 0xfc00fc00u;
+    uint32_t lo[4] = {PINF2, PINF2, PINF2, PINF2}, hi[4] = {NINF2, NINF2, NINF2, NINF2};
+    const float km = pow2f(-ek), vmul = pow2f(-ev);
+    auto h2 = [](uint32_t w) { return *reinterpret_cast<__half2*>(&w); };
+    auto u2 = [](__half2 w) { return *reinterpret_cast<uint32_t*>(&w); };
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      const int t = (u * TEAM + tw) * RPW + sub;
+      if (t < nt) {
+        const size_t off = (size_t)(kept + t) * D + lr * 4;
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint32_t w = qc_codes(x[u][hf * 4] * km, x[u][hf * 4 + 1] * km, x[u][hf * 4 + 2] * km, x[u][hf * 4 + 3] * km);
+          *reinterpret_cast<uint32_t*>(kdst + off + hf * HALF) = w;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const __half2 v = h2(e ? e4m3x2_hi_to_f16x2(w) : e4m3x2_to_f16x2(w));
+            const uint32_t num = u2(v) & __heq2_mask(v, v);        // NaN counts as 0
+            lo[hf * 2 + e] = u2(__hmin2(h2(lo[hf * 2 + e]), h2(num)));
+            hi[hf * 2 + e] = u2(__hmax2(h2(hi[hf * 2 + e]), h2(num)));
+          }
+          const float2 e0 = qc_elems(vraw[u][hf].x, f16), e1 = qc_elems(vraw[u][hf].y, f16);
+          *reinterpret_cast<uint32_t*>(vdst + off + hf * HALF) = qc_codes(e0.x * vmul, e0.y * vmul, e1.x * vmul, e1.y * vmul);
+        }
+      }
+    }
+    if (tw == 0 && lane == 0) *reinterpret_cast<float2*>(c.scales + unit * 2) = make_float2(pow2f(ek), pow2f(ev));
+    if (!c.bounds) continue;
+#pragma unroll
+    for (int o = LPR; o < 32; o <<= 1)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lo[e] = u2(__hmin2(h2(lo[e]), h2(__shfl_xor_sync(0xffffffffu, lo[e], o))));
+        hi[e] = u2(__hmax2(h2(hi[e]), h2(__shfl_xor_sync(0xffffffffu, hi[e], o))));
+      }
+    if (TEAM > 1) {
+      if (sub == 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at2 = lr * 2 + (e & 1) + (e >> 1) * (HALF / 2);
+          s_bnd[warp][0][at2] = lo[e];
+          s_bnd[warp][1][at2] = hi[e];
+        }
+      }
+      team_sync();
+      if (tw == 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at2 = lr * 2 + (e & 1) + (e >> 1) * (HALF / 2);
+          for (int o = 1; o < TEAM; ++o) {
+            lo[e] = u2(__hmin2(h2(lo[e]), h2(s_bnd[team * TEAM + o][0][at2])));
+            hi[e] = u2(__hmax2(h2(hi[e]), h2(s_bnd[team * TEAM + o][1][at2])));
+          }
+        }
+      }
+      team_sync();
+    }
+    if (tw == 0 && sub == 0) {
+      uint8_t* b = c.bounds + unit * 2 * D + lr * 4;
+#pragma unroll
+      for (int side = 0; side < 2; ++side)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          uint32_t* dst = reinterpret_cast<uint32_t*>(b + side * D + hf * HALF);
+          uint32_t w0 = side ? hi[hf * 2] : lo[hf * 2], w1 = side ? hi[hf * 2 + 1] : lo[hf * 2 + 1];
+          if (kept) {                                 // bounds of the rows that were there, in the new scale
+            uint32_t o = *dst;
+            if (ek != ek0) {
+              const float m = pow2f(ek0 - ek);
+              const float2 l2 = qc_half2(e4m3x2_to_f16x2(o)), g2 = qc_half2(e4m3x2_hi_to_f16x2(o));
+              o = qc_codes(l2.x * m, l2.y * m, g2.x * m, g2.y * m);
+            }
+            const __half2 o0 = h2(e4m3x2_to_f16x2(o)), o1 = h2(e4m3x2_hi_to_f16x2(o));
+            w0 = u2(side ? __hmax2(h2(w0), o0) : __hmin2(h2(w0), o0));
+            w1 = u2(side ? __hmax2(h2(w1), o1) : __hmin2(h2(w1), o1));
+          }
+          *dst = f16x4_to_e4m3x4(w0, w1);
+        }
+    }
+  }
+}
+
+// ================================================================================================ select
+constexpr int QS_CHUNK = 128;                // pages a scoring block takes
+constexpr int QS_THREADS = 128;
+constexpr int QS_SEL_THREADS = 512;
+constexpr int QS_CAP = 8192;                 // scores of a unit that the selection keeps in shared memory
+constexpr double QS_UP = 0x1p860, QS_DOWN = 0x1p156;      // QS_UP * QS_DOWN = 2^1016
+
+// a score as an integer of the same order; what is not a number is lowest
+__device__ __forceinline__ unsigned long long qc_key(double x) {
+  if (!(x == x)) return 0ull;
+  const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
+  return (b >> 63) ? ~b : b | 0x8000000000000000ull;
+}
+
+// Scores of QS_CHUNK pages for one (row, KV head).  Both kinds of sums are one dot product of 2 d terms with the page's codes, whatever
+// the group: [sum of min(q, 0), sum of max(q, 0)] . [low, high].  A code's sign and its seven other bits, put where a double has its sign
+// and the low end of its exponent, are that number times 2^-1016 (codes without an exponent included: a subnormal double), so a term is
+// two integer operations and an fp64 multiply-add.  Four lanes take a page, eight pages a warp at a time.
+template <int D>
+__global__ void __launch_bounds__(QS_THREADS)
+qc_score_kernel(const QcDev c, const unsigned short* __restrict__ q, long long q_stride, int Hq, int f16, int keep, int first, int recent,
+                unsigned long long* __restrict__ keys, int chunks, int key_stride) {
+  constexpr int CH = 2 * D / 16;                      // 16-byte pieces of a page's bounds
+  __shared__ double s_w[CH * 18];                     // 16 weights a piece, two apart from the next: no bank twice
+  __shared__ int s_seq;
+  const int chunk = blockIdx.x % chunks, unit = blockIdx.x / chunks, row = unit / c.Hkv, h = unit % c.Hkv, G = Hq / c.Hkv;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int s = qc_seq_of_row(c, row, &s_seq);
+  gp_pdl_launch_dependents();
+  if (s < 0) return;
+  const QcSeq sq = qc_seq(c, s);
+  const int vis = min(sq.slot0 + row - sq.r0 + 1, c.limit);
+  const int m = vis > 0 ? (vis + c.page - 1) >> c.page_log : 0;
+  const int p0 = max(chunk * QS_CHUNK, first), p1 = min((chunk + 1) * QS_CHUNK, m - recent);
+  if (m <= keep || p0 >= p1) return;
+  for (int i = tid; i < D; i += QS_THREADS) {
+    double plus = 0.0, minus = 0.0;
+    for (int g = 0; g < G; ++g) {
+      const double x = qc_elem(q[(size_t)row * q_stride + (size_t)(h * G + g) * D + i], f16 != 0);
+      plus += fmax(x, 0.0); minus += fmin(x, 0.0);
+    }
+    s_w[(i >> 4) * 18 + (i & 15)] = minus * QS_UP;
+    s_w[((i + D) >> 4) * 18 + (i & 15)] = plus * QS_UP;
+  }
+  __syncthreads();
+  const int quad = lane & 3;
+  for (int p = p0 + warp * 8 + (lane >> 2); p - (lane >> 2) < p1; p += QS_THREADS / 4) {
+    const int id = p < p1 ? qc_page(c, s, p) : -1;
+    const size_t u = ((size_t)max(id, 0) * c.Hkv + h);
+    const uint4* src = reinterpret_cast<const uint4*>(c.bounds + u * 2 * D);
+    uint4 w[CH / 4];
+#pragma unroll
+    for (int i = 0; i < CH / 4; ++i) w[i] = src[i * 4 + quad];
+    const float sc = c.scales[u * 2];
+    double acc = 0.0, acc2 = 0.0;
+#pragma unroll
+    for (int i = 0; i < CH / 4; ++i) {
+      const double* ws = s_w + (i * 4 + quad) * 18;
+      const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int b = 0; b < 16; b += 2) {
+        const double2 wt = *reinterpret_cast<const double2*>(ws + b);
+        const uint32_t y0 = word[b >> 2] << (24 - 8 * (b & 3)), y1 = word[b >> 2] << (16 - 8 * (b & 3));
+        acc = fma(__hiloint2double(((int)y0 >> 7) & 0x80fe0000, 0), wt.x, acc);
+        acc2 = fma(__hiloint2double(((int)y1 >> 7) & 0x80fe0000, 0), wt.y, acc2);
+      }
+    }
+    acc += acc2;
+    acc += __shfl_xor_sync(0xffffffffu, acc, 1);
+    acc += __shfl_xor_sync(0xffffffffu, acc, 2);
+    if (quad == 0 && p < p1) keys[(size_t)unit * key_stride + p] = id < 0 ? 0ull : qc_key(acc * QS_DOWN * (double)sc);
+  }
+}
+
+// One block per (row, KV head): the k-th highest key by a radix descent from the first bit in which keys differ, eight bits at a time, then
+// the pages above it and the lowest of those equal to it, in ascending order.
+__global__ void __launch_bounds__(QS_SEL_THREADS)
+qc_select_kernel(const QcDev c, int keep, int first, int recent, const unsigned long long* __restrict__ keys, int key_stride,
+                 int* __restrict__ pages) {
+  extern __shared__ unsigned long long s_key[];
+  __shared__ int s_seq, s_hist[256], s_gt[QS_SEL_THREADS / 32], s_eq[QS_SEL_THREADS / 32], s_bin, s_left, s_count;
+  __shared__ unsigned long long s_lo, s_hi;
+  const int unit = blockIdx.x, row = unit / c.Hkv;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int s = qc_seq_of_row(c, row, &s_seq);
+  gp_pdl_launch_dependents();
+  if (s < 0) { gp_pdl_wait(); return; }
+  const QcSeq sq = qc_seq(c, s);
+  const int vis = min(sq.slot0 + row - sq.r0 + 1, c.limit);
+  const int m = vis > 0 ? (vis + c.page - 1) >> c.page_log : 0;
+  int* out = pages + (size_t)unit * keep;
+  if (m <= keep) {
+    for (int i = tid; i < keep; i += QS_SEL_THREADS) out[i] = i < m ? i : -1;
+    gp_pdl_wait();                                  // no block ends before the kernel in front of it
+    return;
+  }
+  for (int i = tid; i < first; i += QS_SEL_THREADS) out[i] = i;
+  for (int i = tid; i < recent; i += QS_SEL_THREADS) out[keep - recent + i] = m - recent + i;
+  const int want = keep - first - recent, n = m - first - recent;        // want < n
+  gp_pdl_wait();
+  if (want == 0) return;
+  const unsigned long long* src = keys + (size_t)unit * key_stride + first;
+  const bool near = n <= QS_CAP;
+  if (tid == 0) { s_lo = ~0ull; s_hi = 0ull; }
+  __syncthreads();
+  unsigned long long lo = ~0ull, hi = 0ull;
+  for (int i = tid; i < n; i += QS_SEL_THREADS) {
+    const unsigned long long k = src[i];
+    if (near) s_key[i] = k;
+    lo = min(lo, k); hi = max(hi, k);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  if (lane == 0) { atomicMin(&s_lo, lo); atomicMax(&s_hi, hi); }
+  __syncthreads();
+  const unsigned long long* k = near ? s_key : src;
+  // thr: the want-th highest key; ties: how many of its equals are wanted
+  unsigned long long thr = s_lo, known = ~0ull;     // bits of the threshold that are known
+  int left = want;
+  const unsigned long long diff = s_lo ^ s_hi;
+  if (diff) {
+    int top = 64 - __clzll(diff);                   // bits below this one differ
+    known = top == 64 ? 0ull : ~0ull << top;
+    thr = s_hi & known;
+    while (top > 0) {
+      const int bits = min(8, top), sh = top - bits;
+      for (int i = tid; i < 256; i += QS_SEL_THREADS) s_hist[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += QS_SEL_THREADS) {
+        const unsigned long long x = k[i];
+        if ((x & known) == thr) atomicAdd(&s_hist[(int)(x >> sh) & ((1 << bits) - 1)], 1);
+      }
+      __syncthreads();
+      if (warp == 0) {                              // the bin, from above, in which the count passes what is left
+        int cnt[8], sum = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { cnt[e] = s_hist[255 - (lane * 8 + e)]; sum += cnt[e]; }
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += y;
+        }
+        int before = upto - sum;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (before < left && before + cnt[e] >= left) { s_bin = 255 - (lane * 8 + e); s_left = left - before; s_count = cnt[e]; }
+          before += cnt[e];
+        }
+      }
+      __syncthreads();
+      thr |= (unsigned long long)s_bin << sh;
+      known |= (unsigned long long)((1 << bits) - 1) << sh;
+      left = s_left;
+      top = sh;
+      if (s_count == left) break;                   // the whole bin is wanted
+    }
+  }
+  // keys with known bits above thr's, and the first `left` of those equal in them, in order
+  int done = first;                                 // places filled
+  for (int base = 0; base < n; base += QS_SEL_THREADS) {
+    const int i = base + tid;
+    const unsigned long long x = i < n ? (k[i] & known) : 0ull;
+    const bool gt = i < n && x > thr, eq = i < n && x == thr;
+    const unsigned bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
+    __syncthreads();
+    if (lane == 0) { s_gt[warp] = __popc(bg); s_eq[warp] = __popc(be); }
+    __syncthreads();
+    int g0 = 0, e0 = 0, gall = 0, eall = 0;
+#pragma unroll
+    for (int w = 0; w < QS_SEL_THREADS / 32; ++w) {
+      if (w < warp) { g0 += s_gt[w]; e0 += s_eq[w]; }
+      gall += s_gt[w]; eall += s_eq[w];
+    }
+    const unsigned below = (1u << lane) - 1;
+    const int er = e0 + __popc(be & below);         // equals before this one, in this stretch
+    const int at = done + g0 + __popc(bg & below) + min(er, left);
+    if (gt || (eq && er < left)) out[at] = first + i;
+    done += gall + min(eall, left);
+    left -= min(eall, left);
+  }
+}
+
+template <int D>
+struct QcAppendPlan {
+  using K = void (*)(const QcDev, const QcRows, const QcFreq, int, int, int, int, int);
+  K kern;
+  int teams, table_rows;
+};
+// By the new rows a page can receive: few (single tokens, short drafts) leave a warp a head to itself, so that a block's eight warps take
+// eight heads at once; 16 or 32 rows two warps; beyond that all eight warps share a head.  Above 64 rows a table of angles does not fit
+// beside others on an SM; each lane then computes its own.
+template <int D>
+QcAppendPlan<D> qc_append_plan(int rows) {
+  constexpr int RPW = 256 / D;
+  if (rows <= RPW) return {qc_append_kernel<D, 1, 1, true>, 8, RPW};
+  if (rows <= 8 * RPW) return {qc_append_kernel<D, 2, 4, true>, 4, 8 * RPW};
+  if (rows <= 64) return {qc_append_kernel<D, 8, 32 / RPW / 4, true>, 1, 64};
+  if (rows <= 128) return {qc_append_kernel<D, 8, 64 / RPW / 4, false>, 1, 0};
+  return {qc_append_kernel<D, 8, 128 / RPW / 4, false>, 1, 0};
+}
+
+template <int D>
+int qc_append(const QcDev& c, const QcRows& r, const QcFreq& f, cudaStream_t s) {
+  const int rows = c.page < c.max_rows ? c.page : c.max_rows;
+  const QcAppendPlan<D> plan = qc_append_plan<D>(rows);
+  const long long places = ((long long)c.max_rows + c.page - 2) / c.page + 1;      // pages that max_rows new tokens can touch
+  // heads of a page together share the table of angles; apart where that leaves SMs without a block
+  int heads_per = c.Hkv;
+  while (heads_per > plan.teams && places * c.n_seq * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
+  if (heads_per < plan.teams) heads_per = plan.teams;
+  const int groups = (c.Hkv + heads_per - 1) / heads_per;
+  const long long kv = places * c.n_seq * groups;
+  int q_rows = 1;
+  while (q_rows < 16 && c.n_rows / (q_rows * 2) >= 296) q_rows *= 2;
+  const long long qb = r.q ? ((long long)c.n_rows + q_rows - 1) / q_rows : 0;
+  if (kv + qb > 0x7fffffff) return GP_ERR_INVALID;
+  size_t smem = r.rope ? (size_t)plan.table_rows * (D / 2) * sizeof(double2) : 0;
+  const size_t qsmem = r.rope ? (size_t)q_rows * (D / 2) * sizeof(float2) : 0;
+  if (qsmem > smem) smem = qsmem;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(plan.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
+  plan.kern<<<(unsigned)(kv + qb), QA_THREADS, smem, s>>>(c, r, f, (int)places, groups, heads_per, (int)kv, q_rows);
+  return cudaGetLastError() == cudaSuccess ? GP_OK : GP_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" int gp_qcache_append(const gp_qcache* cache, const gp_qbatch* batch, const gp_qrows* rows, void* stream) {
+  QcDev c;
+  const int st = qc_check(cache, batch, &c);
+  if (st != GP_OK) return st;
+  if (!rows || (!qc_empty(c) && (!rows->k || !rows->v)) || (rows->type != GP_TYPE_BF16 && rows->type != GP_TYPE_F16)) return GP_ERR_INVALID;
+  const int64_t need = (int64_t)c.Hkv * cache->head_dim;
+  if (qc_misaligned(rows->k, 16) || qc_misaligned(rows->v, 16) || rows->k_stride < need || rows->v_stride < need || rows->k_stride % 8 || rows->v_stride % 8)
+    return GP_ERR_INVALID;
+  if (qc_misaligned(rows->positions, 4) || qc_misaligned(rows->q_weight, 4) || qc_misaligned(rows->k_weight, 4)) return GP_ERR_INVALID;
+  if (!(rows->eps >= 0.0) || !(rows->rope_theta >= 0.0) || isinf(rows->eps) || isinf(rows->rope_theta)) return GP_ERR_INVALID;
+  if (rows->q) {
+    if (!qc_check_q(cache, rows->q, rows->q_stride, rows->n_q_heads, rows->type)) return GP_ERR_INVALID;
+    if (!rows->q_out || qc_misaligned(rows->q_out, 16) || rows->q_out_stride < (int64_t)rows->n_q_heads * cache->head_dim || rows->q_out_stride % 8)
+      return GP_ERR_INVALID;
+    if (rows->q_out == rows->q && rows->q_out_stride != rows->q_stride) return GP_ERR_INVALID;
+  }
+  if (qc_empty(c)) return GP_OK;
+  QcRows r;
+  r.k = static_cast<const unsigned short*>(rows->k); r.v = static_cast<const unsigned short*>(rows->v);
+  r.q = static_cast<const unsigned short*>(rows->q); r.q_out = static_cast<unsigned short*>(rows->q_out);
+  r.k_stride = rows->k_stride; r.v_stride = rows->v_stride; r.q_stride = rows->q_stride; r.qo_stride = rows->q_out_stride;
+  r.positions = rows->positions;
+  r.qw = rows->q_weight; r.kw = rows->k_weight;
+  r.eps = rows->eps;
+  r.Hq = rows->n_q_heads;
+  r.f16 = rows->type == GP_TYPE_F16;
+  r.rope = rows->rope_theta > 0.0;
+  const int half = cache->head_dim / 2;
+  static thread_local struct { QcFreq f; double theta; int half; } last = {};      // 64 powers take 2 us: kept for the next call with this base
+  if (r.rope && (last.theta != rows->rope_theta || last.half != half)) {
+    for (int i = 0; i < 64; ++i) last.f.over_pi[i] = i < half ? pow(rows->rope_theta, -(double)i / half) / M_PI : 0.0;
+    last.theta = rows->rope_theta; last.half = half;
+  }
+  const QcFreq& f = last.f;
+  QcDevice dev(cache->device);
+  if (!dev.ok) return GP_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return cache->head_dim == 128 ? qc_append<128>(c, r, f, s) : qc_append<64>(c, r, f, s);
+}
+
+extern "C" size_t gp_qcache_select_bytes(const gp_qcache* cache, const gp_qbatch* batch) {
+  QcDev c;
+  if (qc_check(cache, batch, &c) != GP_OK || qc_empty(c)) return 0;
+  return (size_t)c.n_rows * c.Hkv * (((size_t)c.limit + c.page - 1) / c.page) * 8;
+}
+
+extern "C" int gp_qcache_select(const gp_qcache* cache, const gp_qbatch* batch, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t type,
+                                int32_t keep, int32_t first, int32_t recent, int32_t* pages, void* work, size_t work_bytes, void* stream) {
+  QcDev c;
+  const int st = qc_check(cache, batch, &c);
+  if (st != GP_OK) return st;
+  if (!qc_check_q(cache, q, q_stride, n_q_heads, type) || !cache->bounds) return GP_ERR_INVALID;
+  if (keep < 1 || first < 0 || recent < 1 || (int64_t)first + recent > keep || (!qc_empty(c) && (!q || !pages)) || qc_misaligned(pages, 4)) return GP_ERR_INVALID;
+  const size_t need = gp_qcache_select_bytes(cache, batch);
+  if (need && (!work || qc_misaligned(work, 16) || work_bytes < need)) return GP_ERR_INVALID;
+  if (qc_empty(c)) return GP_OK;
+  const long long units = (long long)c.n_rows * c.Hkv;
+  const int stride = (int)(((long long)c.limit + c.page - 1) / c.page);
+  const long long chunks = stride > keep ? (stride + QS_CHUNK - 1) / QS_CHUNK : 0;
+  if (units * (chunks ? chunks : 1) > 0x7fffffff) return GP_ERR_INVALID;
+  QcDevice dev(cache->device);
+  if (!dev.ok) return GP_ERR_CUDA;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  unsigned long long* keys = static_cast<unsigned long long*>(work);
+  if (chunks) {
+    auto score = cache->head_dim == 128 ? qc_score_kernel<128> : qc_score_kernel<64>;
+    score<<<(unsigned)(units * chunks), QS_THREADS, 0, s>>>(c, static_cast<const unsigned short*>(q), q_stride, n_q_heads, type == GP_TYPE_F16, keep, first,
+                                                           recent, keys, (int)chunks, stride);
+    if (cudaGetLastError() != cudaSuccess) return GP_ERR_CUDA;
+  }
+  const size_t smem = (size_t)(stride < QS_CAP ? stride : QS_CAP) * 8;
+  if (smem > 40 * 1024 && cudaFuncSetAttribute(qc_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, QS_CAP * 8) != cudaSuccess) return GP_ERR_CUDA;
+  return gp_launch(qc_select_kernel, (int)units, QS_SEL_THREADS, smem, s, chunks > 0, c, (int)keep, (int)first, (int)recent,
+                   static_cast<const unsigned long long*>(keys), stride, static_cast<int*>(pages)) == cudaSuccess ? GP_OK : GP_ERR_CUDA;
+}
