@@ -492,6 +492,8 @@ class QBatch:
         self.n_rows = n_rows
         self.desc = gp_qbatch(row_start.data_ptr(), seq_len.data_ptr(), page_table.data_ptr(), n_seq, page_table.shape[1], n_rows, max_rows,
                               max_len, 0)
+        self.ref = C.byref(self.desc)
+        self.work = {}                                     # bytes of work memory, by what they depend on beside this description
 
 
 class QCache:
@@ -517,6 +519,9 @@ class QCache:
         self.n_kv_heads, self.head_dim, self.page_size = heads, d, page
         self.desc = gp_qcache(heads, d, page, codes.device.index, n_pages, codes.data_ptr(), scales.data_ptr(),
                               bounds.data_ptr() if bounds is not None else None, status.data_ptr() if status is not None else None)
+        self._ref, self._lib, self._index = C.byref(self.desc), lib(), codes.device.index
+        self._raw_stream = torch._C._cuda_getCurrentRawStream      # the current stream's handle, without an object around it
+        self._shape, self._checked = (heads, d, page), {}
 
     @classmethod
     def create(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 16, device: int = 0, bounds: bool = True) -> "QCache":
@@ -530,10 +535,15 @@ class QCache:
                    f8(n_pages, n_kv_heads, 2, head_dim) if bounds else None, torch.zeros(1, dtype=torch.int32, **kw))
 
     def stream(self) -> int:
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self._index)
 
     def _rows(self, name: str, t, batch: QBatch, heads: int, dtype=None) -> int:
-        """Checks a [n_rows][heads][head_dim] tensor whose rows may be apart; returns the distance between them."""
+        """Checks a [n_rows][heads][head_dim] tensor whose rows may be apart; returns the distance between them.  (Checked once per
+        shape, strides and type: the checks cost as much as a launch.)"""
+        key = (t.shape, t.stride(), t.dtype, t.device, batch.n_rows, batch.device, heads, dtype)
+        stride = self._checked.get(key)
+        if stride is not None:
+            return stride
         if t.dim() != 3 or t.shape[0] != batch.n_rows or t.shape[2] != self.head_dim or (heads and t.shape[1] != heads):
             raise ValueError(f"{name}: [n_rows][heads][head_dim] is needed")
         if t.device != self.device or batch.device != self.device:
@@ -543,29 +553,38 @@ class QCache:
         stride, head, elem = t.stride()
         if elem != 1 or (head != self.head_dim and t.shape[1] > 1):
             raise ValueError(f"{name}: the heads of a row lie one behind the other")
-        return max(stride, t.shape[1] * self.head_dim) if batch.n_rows <= 1 else stride
+        if batch.n_rows <= 1:
+            stride = max(stride, t.shape[1] * self.head_dim)
+        if len(self._checked) > 1000:
+            self._checked.clear()
+        self._checked[key] = stride
+        return stride
 
     def append(self, batch: QBatch, k, v, q=None, q_out=None, positions=None, rope_theta: float = 0.0, q_weight=None, k_weight=None,
                eps: float = 1e-6):
         """Puts the batch's rows into the cache (gp_qcache_append); returns the normalised and rotated queries (q_out, a new tensor where
         none is given), or None without q."""
         torch = self.torch
-        rows = gp_qrows(k=k.data_ptr(), v=v.data_ptr(), k_stride=self._rows("k", k, batch, self.n_kv_heads),
-                        v_stride=self._rows("v", v, batch, self.n_kv_heads, k.dtype), eps=eps, rope_theta=rope_theta, type=self._types[k.dtype])
-        for name, t, dtype, n in (("positions", positions, torch.int32, batch.n_rows), ("q_weight", q_weight, torch.float32, self.head_dim),
-                                  ("k_weight", k_weight, torch.float32, self.head_dim)):
-            if t is not None:
-                if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.device:
-                    raise ValueError(f"{name}: a contiguous {dtype} tensor of {n} on the cache's device is needed")
-                setattr(rows, name, t.data_ptr())
+        dtype = k.dtype
+        ks, vs = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads, dtype)
+        for name, t, kind, n in (("positions", positions, torch.int32, batch.n_rows), ("q_weight", q_weight, torch.float32, self.head_dim),
+                                 ("k_weight", k_weight, torch.float32, self.head_dim)):
+            if t is not None and (t.dtype != kind or t.numel() != n or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"{name}: a contiguous {kind} tensor of {n} on the cache's device is needed")
+        q_ptr = out_ptr = None
+        qs = os_ = heads = 0
         if q is not None:
-            rows.q, rows.q_stride, rows.n_q_heads = q.data_ptr(), self._rows("q", q, batch, 0, k.dtype), q.shape[1]
+            heads = q.shape[1]
+            q_ptr, qs = q.data_ptr(), self._rows("q", q, batch, 0, dtype)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=self.device)
-            rows.q_out, rows.q_out_stride = q_out.data_ptr(), self._rows("q_out", q_out, batch, q.shape[1], k.dtype)
+                q_out = torch.empty(q.shape, dtype=dtype, device=self.device)
+            out_ptr, os_ = q_out.data_ptr(), self._rows("q_out", q_out, batch, heads, dtype)
         elif q_out is not None:
             raise ValueError("q_out without q")
-        gp_qcache_append(self.desc, batch.desc, rows, self.stream())
+        rows = gp_qrows(k.data_ptr(), v.data_ptr(), q_ptr, out_ptr, ks, vs, qs, os_, None if positions is None else positions.data_ptr(),
+                        None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps, rope_theta,
+                        heads, self._types[dtype])
+        _check(self._lib.gp_qcache_append(self._ref, batch.ref, C.byref(rows), self._raw_stream(self._index)), "gp_qcache_append")
         return q_out
 
     def attention(self, batch: QBatch, q, out=None, out_dtype=None, pages=None):
@@ -574,21 +593,26 @@ class QCache:
         stride = self._rows("q", q, batch, 0)
         if out is None:
             out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
-        elif tuple(out.shape) != tuple(q.shape) or not out.is_contiguous() or out.device != self.device or (out_dtype or out.dtype) != out.dtype:
+        elif out.shape != q.shape or not out.is_contiguous() or out.device != self.device or (out_dtype or out.dtype) != out.dtype:
             raise ValueError("out: a contiguous tensor of the queries' shape on the cache's device is needed")
-        if out.dtype not in self._types:
+        out_type = self._types.get(out.dtype)
+        if out_type is None:
             raise ValueError("out: bfloat16, float16 or float32 is needed")
-        n_list = 0
+        n_list, pages_ptr = 0, None
         if pages is not None:
-            n_list = pages.shape[-1]
-            if pages.dtype != torch.int32 or tuple(pages.shape) != (batch.n_rows, self.n_kv_heads, n_list) or n_list < 1 or \
+            n_list, pages_ptr = pages.shape[-1], pages.data_ptr()
+            if pages.dtype != torch.int32 or pages.shape != (batch.n_rows, self.n_kv_heads, n_list) or n_list < 1 or \
                     not pages.is_contiguous() or pages.device != self.device:
                 raise ValueError("pages: a contiguous int32 tensor [n_rows][n_kv_heads][n_list] on the cache's device is needed")
-        need = gp_qcache_attention_bytes(self.desc, batch.desc, q.shape[1], n_list)
+        heads = q.shape[1]
+        key = (self._shape, heads, n_list)
+        need = batch.work.get(key)
+        if need is None:
+            need = batch.work[key] = self._lib.gp_qcache_attention_bytes(self._ref, batch.ref, heads, n_list)
         work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        gp_qcache_attention(self.desc, batch.desc, q.data_ptr(), stride, q.shape[1], self._types[q.dtype],
-                            pages.data_ptr() if n_list else None, n_list, out.data_ptr(), self._types[out.dtype],
-                            work.data_ptr() if need else None, need, self.stream())
+        _check(self._lib.gp_qcache_attention(self._ref, batch.ref, q.data_ptr(), stride, heads, self._types[q.dtype], pages_ptr, n_list,
+                                             out.data_ptr(), out_type, work.data_ptr() if need else None, need,
+                                             self._raw_stream(self._index)), "gp_qcache_attention")
         return out
 
     def select(self, batch: QBatch, q, keep: int, first: int = 1, recent: int = 1, pages=None):
@@ -598,12 +622,16 @@ class QCache:
         shape = (batch.n_rows, self.n_kv_heads, keep)
         if pages is None:
             pages = torch.empty(shape, dtype=torch.int32, device=self.device)
-        elif pages.dtype != torch.int32 or tuple(pages.shape) != shape or not pages.is_contiguous() or pages.device != self.device:
+        elif pages.dtype != torch.int32 or pages.shape != shape or not pages.is_contiguous() or pages.device != self.device:
             raise ValueError(f"pages: a contiguous int32 tensor {shape} on the cache's device is needed")
-        need = gp_qcache_select_bytes(self.desc, batch.desc)
+        key = (self._shape, "select")
+        need = batch.work.get(key)
+        if need is None:
+            need = batch.work[key] = self._lib.gp_qcache_select_bytes(self._ref, batch.ref)
         work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        gp_qcache_select(self.desc, batch.desc, q.data_ptr(), stride, q.shape[1], self._types[q.dtype], keep, first, recent, pages.data_ptr(),
-                         work.data_ptr() if need else None, need, self.stream())
+        _check(self._lib.gp_qcache_select(self._ref, batch.ref, q.data_ptr(), stride, q.shape[1], self._types[q.dtype], keep, first, recent,
+                                          pages.data_ptr(), work.data_ptr() if need else None, need, self._raw_stream(self._index)),
+               "gp_qcache_select")
         return pages
 
 

@@ -12,8 +12,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgrowpage.so")
-SOURCES = ["gp_pool.cu", "gp_attn.cu", "gp_boundary.cu", "gp_noalloc.cu", "gp_qcache.cu", "gp_qattn.cu"]
-HEADERS = ["gp_dev.cuh", "gp_qcache.cuh", os.path.join("..", "..", "include", "growpage.h")]
+SOURCES = ["gp_pool.cu", "gp_attn.cu", "gp_boundary.cu", "gp_noalloc.cu", "gp_qcache.cu", "gp_qattn.cu", "gp_qprompt.cu"]
+HEADERS = ["gp_dev.cuh", "gp_qcache.cuh", "gp_qattn.cuh", "gp_qprompt.cuh", os.path.join("..", "..", "include", "growpage.h")]
 
 
 def _nvcc() -> str:
@@ -35,7 +35,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "--threads", "6", "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
+           "--threads", "7", "-shared", "-Xcompiler", "-fPIC", "-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

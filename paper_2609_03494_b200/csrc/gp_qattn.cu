@@ -2,12 +2,10 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
-#include "gp_qcache.cuh"
+#include "gp_qprompt.cuh"
 
 namespace {
 
-constexpr int QT_WARPS = 4;
-constexpr int QT_THREADS = QT_WARPS * 32;
 constexpr int QT_STAGES = 2;                   // stages of a warp's ring
 constexpr int QT_TILES = 2;                    // tiles of 16 tokens in a stage
 constexpr int QT_GRANULE = QT_WARPS * QT_TILES * 16;
@@ -17,17 +15,6 @@ constexpr float QT_LIFT = 8.f;                 // weights are carried times 2^8 
 constexpr float QT_SLACK = 7.f;                // ... while no logit is further above the maximum they refer to than this (base 2)
 
 constexpr int qt_resident(int nt, int d) { return nt * d <= 128 ? 3 : 2; }      // blocks of an SM that the registers allow
-
-struct QtArgs {
-  const unsigned short* q;
-  long long q_stride;
-  int Hq, G, f16;
-  const int* pages; int n_list;                // nullptr: all pages
-  void* out; int out_type;
-  int4* joins;                                 // [blocks][2] what qt_merge_kernel has to do
-  float* part;                                 // [blocks][2][columns][D + 2]
-  int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
-};
 
 // D(16x8, fp32) += A(16x16, fp16, row) * B(16x8, fp16, col)
 __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -47,29 +34,9 @@ __device__ __forceinline__ void qt_tma_rows(uint32_t dst_smem, const CUtensorMap
                "r"(0), "r"(row), "r"(page), "r"(bar)
                : "memory");
 }
-__device__ __forceinline__ float qt_exp2(float x) {      // 2^x to 2^-22 relative; 0 below 2^-126
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ void qt_store(void* out, int type, size_t i, float x) {
-  if (type == GP_TYPE_F32) static_cast<float*>(out)[i] = x;
-  else if (type == GP_TYPE_F16) static_cast<__half*>(out)[i] = __float2half_rn(x);
-  else static_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(x);
-}
-
 // The work of a call is one line of granules (the tokens that a block's warps take at a time): sequence by sequence, KV head by KV head, tile of
 // rows by tile of rows.  Every thread block takes the same stretch of it, whatever the lengths: none waits for a long sequence at the end, and
 // only the first and the last unit of a stretch can be shared with other blocks, so two partial results per block are all there is.
-struct QtUnit {
-  int seq, h, row0, rows, cols, slot0;         // of the tile: first batch row, rows, columns, slot of the first row
-  int t0, t1;                                  // tokens of the stretch (with a list: places of the list times the page size)
-  int total;                                   // granules of the unit, on the line behind QT_UNIT more
-};
-// tokens that column `col` of a unit sees
-__device__ __forceinline__ int qt_visible(const QcDev& c, const QtUnit& u, int G, int col) {
-  return min(u.slot0 + col / G + 1, c.limit);
-}
 template <bool LIST>
 __device__ __forceinline__ int qt_granules(const QcDev& c, const QtArgs& a, const QcSeq& q, int tile) {      // of one unit
   if (LIST) return ((a.n_list << c.page_log) + QT_GRANULE - 1) / QT_GRANULE;
@@ -82,83 +49,6 @@ __device__ __forceinline__ long long qt_head_granules(const QcDev& c, const QtAr
   long long g = 0;
   for (int t = 0; t * a.rows_tile < q.rows; ++t) g += qt_granules<LIST>(c, a, q, t) + QT_UNIT;
   return g;
-}
-
-// Joins the parts of a column: weights 2^(m - max).  p: [parts][stride] floats of a part's column: D values, m, sum.
-template <int D>
-__device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, float* part) {
-  constexpr int ST = D + 2;
-  for (int i = threadIdx.x; i < u.cols * D; i += QT_THREADS) {
-    const int col = i / D, e = i % D;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) M = fmaxf(M, s_part[(size_t)(w * cols_stride + col) * ST + D]);
-    float o = 0.f, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) {
-      const float* p = s_part + (size_t)(w * cols_stride + col) * ST;
-      const float wt = M == -INFINITY ? 0.f : exp2f(p[D] - M);
-      o += wt * p[e];
-      l += wt * p[D + 1];
-    }
-    if (!part) {
-      const size_t rh = (size_t)(u.row0 + col / a.G) * a.Hq + u.h * a.G + col % a.G;
-      qt_store(a.out, a.out_type, rh * D + e, l != 0.f ? o / l : 0.f);      // (a NaN sum is not 0)
-    } else {
-      float* dst = part + (size_t)col * ST;
-      dst[e] = o;
-      if (e == 0) { dst[D] = M; dst[D + 1] = l; }
-    }
-  }
-}
-
-// The unit in plain arithmetic, a warp a token and column after column: for a result that is not finite where rows see different tokens (a
-// NaN value that one row sees must not reach another through a weight of zero).
-template <int D>
-__device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part) {
-  constexpr int PER = D / 32, ST = D + 2;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const float scale = 1.4426950408889634f * rsqrtf((float)D);
-  for (int col = 0; col < u.cols; ++col) {
-    const int row = u.row0 + col / a.G, head = u.h * a.G + col % a.G, vis = qt_visible(c, u, a.G, col);
-    float q[PER], o[PER], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) { q[e] = qc_elem(a.q[(size_t)row * a.q_stride + (size_t)head * D + lane + 32 * e], a.f16); o[e] = 0.f; }
-    for (int t = u.t0 + warp; t < min(u.t1, vis); t += QT_WARPS) {
-      const int id = qc_page(c, u.seq, t >> c.page_log);
-      if (id < 0) continue;
-      const size_t unit = (size_t)id * c.Hkv + u.h;
-      const uint8_t* kp = c.codes + (unit * 2 * c.page + (t & (c.page - 1))) * D;
-      const uint8_t* vp = kp + (size_t)c.page * D;
-      const float2 sc = *reinterpret_cast<const float2*>(c.scales + unit * 2);
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) s += q[e] * (qc_half2(e4m3x2_to_f16x2(kp[lane + 32 * e])).x * sc.x);
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-      s *= scale;
-      const float mn = fmaxf(m, s), corr = m == mn ? 1.f : exp2f(m - mn), p = exp2f(s - mn);
-      l = l * corr + p;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] = o[e] * corr + p * (qc_half2(e4m3x2_to_f16x2(vp[lane + 32 * e])).x * sc.y);
-      m = mn;
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) smem[warp * ST + lane + 32 * e] = o[e];
-    if (lane == 0) { smem[warp * ST + D] = m; smem[warp * ST + D + 1] = l; }
-    __syncthreads();
-    QtUnit one = u;
-    one.cols = 1; one.row0 = row;
-    if (!part) {                                        // qt_write's column 0 is this head
-      QtArgs b = a;
-      b.G = 1; b.Hq = 1;
-      one.row0 = row * a.Hq + head; one.h = 0;
-      qt_write<D>(b, one, smem, 1, nullptr);
-    } else {
-      qt_write<D>(a, one, smem, 1, part + (size_t)col * ST);
-    }
-    __syncthreads();
-  }
 }
 
 // A column is a (row, query head of the group); NT tiles of eight columns share the keys and values that a block brings in.  Tokens are the rows
@@ -541,46 +431,6 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
   if (gave_up && c.status) atomicOr(c.status, GP_E_SPIN);
 }
 
-// One block per (block of the kernel before, column): joins the parts of the unit that ended in that block's stretch, if it began before.
-template <int D, int COLS>
-__global__ void __launch_bounds__(D)
-qt_merge_kernel(const QtArgs a) {
-  __shared__ float s_w[256], s_l[256], s_red[D / 32];
-  constexpr int ST = D + 2;
-  const int tid = threadIdx.x, col = blockIdx.x % COLS, b = blockIdx.x / COLS;
-  gp_pdl_wait();
-  const int4 j = __ldcg(a.joins + b * 2);              // columns, the first part, the next block, the last block
-  if (col >= j.x) return;
-  const int4 u = __ldcg(a.joins + b * 2 + 1);
-  const int n_parts = j.w - j.z + 2;
-  auto part = [&](int s) { return a.part + ((size_t)(s == 0 ? j.y : (j.z + s - 1) * 2) * COLS + col) * ST; };
-  float M = -INFINITY;
-  for (int s = tid; s < n_parts; s += D) M = fmaxf(M, __ldcg(part(s) + D));
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-  if ((tid & 31) == 0) s_red[tid >> 5] = M;
-  __syncthreads();
-  for (int w = 0; w < D / 32; ++w) M = fmaxf(M, s_red[w]);
-  float o = 0.f, l = 0.f;
-  for (int s0 = 0; s0 < n_parts; s0 += 256) {
-    const int n = min(256, n_parts - s0);
-    __syncthreads();
-    for (int s = tid; s < n; s += D) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(s0 + s) + D));
-      s_w[s] = M == -INFINITY ? 0.f : exp2f(ml.x - M);
-      s_l[s] = ml.y;
-    }
-    __syncthreads();
-#pragma unroll 8
-    for (int s = 0; s < n; ++s) {
-      o += s_w[s] * __ldcg(part(s0 + s) + tid);
-      l += s_w[s] * s_l[s];
-    }
-  }
-  const size_t rh = (size_t)(u.x + col / a.G) * a.Hq + u.y * a.G + col % a.G;
-  qt_store(a.out, a.out_type, rh * D + tid, l != 0.f ? o / l : 0.f);
-}
-
 // The codes as TMA sees them: [pages][rows of a page: KV head, keys | values, token][d], 16 rows at a time, swizzled so that ldmatrix meets no
 // bank twice.  Encoded anew for every call (host work of a fraction of a microsecond).
 bool qt_map(const gp_qcache* c, CUtensorMap* map) {
@@ -598,6 +448,9 @@ bool qt_map(const gp_qcache* c, CUtensorMap* map) {
                 d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Whether the kernel for many rows takes the call.
+bool qt_many_rows(const QcDev& c, int G, bool list) { return !list && (long long)c.max_rows * G > 64; }
 
 // How a call is cut up, by sizes alone.
 struct QtPlan { int nt, blocks; };
@@ -626,7 +479,7 @@ int qt_launch(const QcDev& c, const QtArgs& a, const CUtensorMap& map, const QtP
   smem += 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
   if (gp_launch(kern, p.blocks, QT_THREADS, smem, s, LIST, c, a, map) != cudaSuccess) return GP_ERR_CUDA;
-  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, NT * 8>, p.blocks * NT * 8, D, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
+  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, NT * 8, 2>, p.blocks * NT * 8, D, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
   return GP_OK;
 }
 template <int D, int TERMS>
@@ -646,7 +499,9 @@ extern "C" size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qba
   QcDev c;
   if (qc_check(cache, batch, &c) != GP_OK || n_q_heads < 1 || n_q_heads % c.Hkv || n_q_heads / c.Hkv > 8 || n_list < 0) return 0;
   if (qc_empty(c)) return 0;
-  return qt_bytes(qt_plan(c, n_q_heads / c.Hkv, cache->head_dim, n_list, n_list > 0), cache->head_dim);
+  const int G = n_q_heads / c.Hkv;
+  if (qt_many_rows(c, G, n_list > 0)) return qp_bytes(qp_plan(c, G), cache->head_dim);
+  return qt_bytes(qt_plan(c, G, cache->head_dim, n_list, n_list > 0), cache->head_dim);
 }
 
 extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batch, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t type,
@@ -664,6 +519,14 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
   a.Hq = n_q_heads; a.G = n_q_heads / c.Hkv; a.f16 = type == GP_TYPE_F16;
   a.pages = pages; a.n_list = n_list;
   a.out = out; a.out_type = out_type;
+  const bool many = qt_many_rows(c, a.G, pages != nullptr);
+  if (many) {
+    const QpPlan p = qp_plan(c, a.G);
+    const size_t need = qp_bytes(p, cache->head_dim);
+    if (need && (!work || qc_misaligned(work, 16) || work_bytes < need)) return GP_ERR_INVALID;
+    QcDevice dev(cache->device);
+    return dev.ok ? qp_launch(c, a, p, cache->head_dim, work, static_cast<cudaStream_t>(stream)) : GP_ERR_CUDA;
+  }
   const QtPlan p = qt_plan(c, a.G, cache->head_dim, n_list, pages != nullptr);
   if (!work || qc_misaligned(work, 16) || work_bytes < qt_bytes(p, cache->head_dim)) return GP_ERR_INVALID;
   a.joins = static_cast<int4*>(work);

@@ -1,0 +1,158 @@
+// What the two attention kernels of the 8-bit cache share: arguments, units of work, how warps' and blocks' parts of a result are joined.
+#pragma once
+#include "gp_qcache.cuh"
+
+constexpr int QT_WARPS = 4;
+constexpr int QT_THREADS = QT_WARPS * 32;
+
+struct QtArgs {
+  const unsigned short* q;
+  long long q_stride;
+  int Hq, G, f16;
+  const int* pages; int n_list;                // nullptr: all pages
+  void* out; int out_type;
+  int4* joins;                                 // [blocks][2] what qt_merge_kernel has to do
+  float* part;                                 // [blocks][2][columns][D + 2]
+  int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
+};
+
+__device__ __forceinline__ float qt_exp2(float x) {      // 2^x to 2^-22 relative; 0 below 2^-126
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void qt_store(void* out, int type, size_t i, float x) {
+  if (type == GP_TYPE_F32) static_cast<float*>(out)[i] = x;
+  else if (type == GP_TYPE_F16) static_cast<__half*>(out)[i] = __float2half_rn(x);
+  else static_cast<__nv_bfloat16*>(out)[i] = __float2bfloat16_rn(x);
+}
+
+struct QtUnit {
+  int seq, h, row0, rows, cols, slot0;         // of the tile: first batch row, rows, columns, slot of the first row
+  int t0, t1;                                  // tokens of the stretch (with a list: places of the list times the page size)
+  int total;                                   // granules of the unit, on the line behind QT_UNIT more
+};
+// tokens that column `col` of a unit sees
+__device__ __forceinline__ int qt_visible(const QcDev& c, const QtUnit& u, int G, int col) {
+  return min(u.slot0 + col / G + 1, c.limit);
+}
+// The first four warps of a block (all of it, in the kernel that has no more) meet.
+__device__ __forceinline__ void qt_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// Joins the parts of a column: weights 2^(m - max).  p: [parts][stride] floats of a part's column: D values, m, sum.
+template <int D>
+__device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, float* part) {
+  constexpr int ST = D + 2;
+  for (int i = threadIdx.x; i < u.cols * D; i += QT_THREADS) {
+    const int col = i / D, e = i % D;
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) M = fmaxf(M, s_part[(size_t)(w * cols_stride + col) * ST + D]);
+    float o = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) {
+      const float* p = s_part + (size_t)(w * cols_stride + col) * ST;
+      const float wt = M == -INFINITY ? 0.f : exp2f(p[D] - M);
+      o += wt * p[e];
+      l += wt * p[D + 1];
+    }
+    if (!part) {
+      const size_t rh = (size_t)(u.row0 + col / a.G) * a.Hq + u.h * a.G + col % a.G;
+      qt_store(a.out, a.out_type, rh * D + e, l != 0.f ? o / l : 0.f);      // (a NaN sum is not 0)
+    } else {
+      float* dst = part + (size_t)col * ST;
+      dst[e] = o;
+      if (e == 0) { dst[D] = M; dst[D + 1] = l; }
+    }
+  }
+}
+
+// The unit in plain arithmetic, a warp a token and column after column: for a result that is not finite where rows see different tokens (a
+// NaN value that one row sees must not reach another through a weight of zero).
+template <int D>
+__device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part) {
+  constexpr int PER = D / 32, ST = D + 2;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float scale = 1.4426950408889634f * rsqrtf((float)D);
+  for (int col = 0; col < u.cols; ++col) {
+    const int row = u.row0 + col / a.G, head = u.h * a.G + col % a.G, vis = qt_visible(c, u, a.G, col);
+    float q[PER], o[PER], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) { q[e] = qc_elem(a.q[(size_t)row * a.q_stride + (size_t)head * D + lane + 32 * e], a.f16); o[e] = 0.f; }
+    for (int t = u.t0 + warp; t < min(u.t1, vis); t += QT_WARPS) {
+      const int id = qc_page(c, u.seq, t >> c.page_log);
+      if (id < 0) continue;
+      const size_t unit = (size_t)id * c.Hkv + u.h;
+      const uint8_t* kp = c.codes + (unit * 2 * c.page + (t & (c.page - 1))) * D;
+      const uint8_t* vp = kp + (size_t)c.page * D;
+      const float2 sc = *reinterpret_cast<const float2*>(c.scales + unit * 2);
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) s += q[e] * (qc_half2(e4m3x2_to_f16x2(kp[lane + 32 * e])).x * sc.x);
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+      s *= scale;
+      const float mn = fmaxf(m, s), corr = m == mn ? 1.f : exp2f(m - mn), p = exp2f(s - mn);
+      l = l * corr + p;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[e] = o[e] * corr + p * (qc_half2(e4m3x2_to_f16x2(vp[lane + 32 * e])).x * sc.y);
+      m = mn;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) smem[warp * ST + lane + 32 * e] = o[e];
+    if (lane == 0) { smem[warp * ST + D] = m; smem[warp * ST + D + 1] = l; }
+    qt_sync();
+    QtUnit one = u;
+    one.cols = 1; one.row0 = row;
+    if (!part) {                                        // qt_write's column 0 is this head
+      QtArgs b = a;
+      b.G = 1; b.Hq = 1;
+      one.row0 = row * a.Hq + head; one.h = 0;
+      qt_write<D>(b, one, smem, 1, nullptr);
+    } else {
+      qt_write<D>(a, one, smem, 1, part + (size_t)col * ST);
+    }
+    qt_sync();
+  }
+}
+
+// One block per (block of the kernel before, column): joins the parts of the unit that ended in that block's stretch, if it began before.
+template <int D, int COLS, int SLOTS>      // SLOTS: partial results a block has room for
+__global__ void __launch_bounds__(D)
+qt_merge_kernel(const QtArgs a) {
+  __shared__ float s_w[256], s_l[256], s_red[D / 32];
+  constexpr int ST = D + 2;
+  const int tid = threadIdx.x, col = blockIdx.x % COLS, b = blockIdx.x / COLS;
+  gp_pdl_wait();
+  const int4 j = __ldcg(a.joins + b * 2);              // columns, the first part, the next block, the last block
+  if (col >= j.x) return;
+  const int4 u = __ldcg(a.joins + b * 2 + 1);
+  const int n_parts = j.w - j.z + 2;
+  auto part = [&](int s) { return a.part + ((size_t)(s == 0 ? j.y : (j.z + s - 1) * SLOTS) * COLS + col) * ST; };
+  float M = -INFINITY;
+  for (int s = tid; s < n_parts; s += D) M = fmaxf(M, __ldcg(part(s) + D));
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+  if ((tid & 31) == 0) s_red[tid >> 5] = M;
+  __syncthreads();
+  for (int w = 0; w < D / 32; ++w) M = fmaxf(M, s_red[w]);
+  float o = 0.f, l = 0.f;
+  for (int s0 = 0; s0 < n_parts; s0 += 256) {
+    const int n = min(256, n_parts - s0);
+    __syncthreads();
+    for (int s = tid; s < n; s += D) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(s0 + s) + D));
+      s_w[s] = M == -INFINITY ? 0.f : exp2f(ml.x - M);
+      s_l[s] = ml.y;
+    }
+    __syncthreads();
+#pragma unroll 8
+    for (int s = 0; s < n; ++s) {
+      o += s_w[s] * __ldcg(part(s0 + s) + tid);
+      l += s_w[s] * s_l[s];
+    }
+  }
+  const size_t rh = (size_t)(u.x + col / a.G) * a.Hq + u.y * a.G + col % a.G;
+  qt_store(a.out, a.out_type, rh * D + tid, l != 0.f ? o / l : 0.f);
+}
+
