@@ -406,7 +406,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
           for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[n][j][e]) < INFINITY) && n * 8 + (lane & 3) * 2 + (e & 1) < u.cols;
     }
     if (__syncthreads_or(u.rows > 1 && bad)) {
-      qt_plain<D>(c, a, u, reinterpret_cast<float*>(smem), part);
+      qt_plain<D>(c, a, u, reinterpret_cast<float*>(smem), part, 1);
     } else {
       float* s_part = reinterpret_cast<float*>(smem);   // [warps][NT * 8][D + 2]
 #pragma unroll

@@ -36,14 +36,14 @@ struct QtUnit {
 __device__ __forceinline__ int qt_visible(const QcDev& c, const QtUnit& u, int G, int col) {
   return min(u.slot0 + col / G + 1, c.limit);
 }
-// The first four warps of a block (all of it, in the kernel that has no more) meet.
-__device__ __forceinline__ void qt_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// Four warps of a block (all of it, in the kernel that has no more) meet.
+__device__ __forceinline__ void qt_sync(int bar) { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); }
 
 // Joins the parts of a column: weights 2^(m - max).  p: [parts][stride] floats of a part's column: D values, m, sum.
 template <int D>
 __device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, float* part) {
   constexpr int ST = D + 2;
-  for (int i = threadIdx.x; i < u.cols * D; i += QT_THREADS) {
+  for (int i = threadIdx.x % QT_THREADS; i < u.cols * D; i += QT_THREADS) {
     const int col = i / D, e = i % D;
     float M = -INFINITY;
 #pragma unroll
@@ -70,9 +70,9 @@ __device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const
 // The unit in plain arithmetic, a warp a token and column after column: for a result that is not finite where rows see different tokens (a
 // NaN value that one row sees must not reach another through a weight of zero).
 template <int D>
-__device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part) {
+__device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part, int bar) {
   constexpr int PER = D / 32, ST = D + 2;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = (threadIdx.x >> 5) % QT_WARPS, lane = threadIdx.x & 31;
   const float scale = 1.4426950408889634f * rsqrtf((float)D);
   for (int col = 0; col < u.cols; ++col) {
     const int row = u.row0 + col / a.G, head = u.h * a.G + col % a.G, vis = qt_visible(c, u, a.G, col);
@@ -101,7 +101,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
 #pragma unroll
     for (int e = 0; e < PER; ++e) smem[warp * ST + lane + 32 * e] = o[e];
     if (lane == 0) { smem[warp * ST + D] = m; smem[warp * ST + D + 1] = l; }
-    qt_sync();
+    qt_sync(bar);
     QtUnit one = u;
     one.cols = 1; one.row0 = row;
     if (!part) {                                        // qt_write's column 0 is this head
@@ -112,7 +112,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
     } else {
       qt_write<D>(a, one, smem, 1, part + (size_t)col * ST);
     }
-    qt_sync();
+    qt_sync(bar);
   }
 }
 

@@ -2,7 +2,7 @@
 #pragma once
 #include "gp_qattn.cuh"
 
-struct QpPlan { int rows_tile, tiles, n_split; long long blocks; };
+struct QpPlan { int blocks; };
 QpPlan qp_plan(const QcDev& c, int G);
 size_t qp_bytes(const QpPlan& p, int d);
 int qp_launch(const QcDev& c, QtArgs a, const QpPlan& p, int d, void* work, cudaStream_t s);
