@@ -479,7 +479,7 @@ int qt_launch(const QcDev& c, const QtArgs& a, const CUtensorMap& map, const QtP
   smem += 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
   if (gp_launch(kern, p.blocks, QT_THREADS, smem, s, LIST, c, a, map) != cudaSuccess) return GP_ERR_CUDA;
-  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, NT * 8, 2>, p.blocks * NT * 8, D, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
+  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, NT * 8, 2>, p.blocks * NT * 2, 128, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
   return GP_OK;
 }
 template <int D, int TERMS>

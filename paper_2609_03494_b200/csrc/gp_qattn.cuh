@@ -116,43 +116,56 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
   }
 }
 
-// One block per (block of the kernel before, column): joins the parts of the unit that ended in that block's stretch, if it began before.
+// A warp per (block of the kernel before, column): joins the parts of the unit that ended in that block's stretch, if it began before.  (A block per
+// column cost the kernel for many rows 38 000 blocks, nearly all without work.)
 template <int D, int COLS, int SLOTS>      // SLOTS: partial results a block has room for
-__global__ void __launch_bounds__(D)
-qt_merge_kernel(const QtArgs a) {
-  __shared__ float s_w[256], s_l[256], s_red[D / 32];
-  constexpr int ST = D + 2;
-  const int tid = threadIdx.x, col = blockIdx.x % COLS, b = blockIdx.x / COLS;
+__global__ void __launch_bounds__(128)
+qt_merge_kernel(const __grid_constant__ QtArgs a) {
+  constexpr int ST = D + 2, PER = D / 64;               // pairs of elements a lane
+  const int lane = threadIdx.x & 31, at = blockIdx.x * 4 + (threadIdx.x >> 5), col = at % COLS, b = at / COLS;
   gp_pdl_wait();
   const int4 j = __ldcg(a.joins + b * 2);              // columns, the first part, the next block, the last block
   if (col >= j.x) return;
   const int4 u = __ldcg(a.joins + b * 2 + 1);
   const int n_parts = j.w - j.z + 2;
   auto part = [&](int s) { return a.part + ((size_t)(s == 0 ? j.y : (j.z + s - 1) * SLOTS) * COLS + col) * ST; };
-  float M = -INFINITY;
-  for (int s = tid; s < n_parts; s += D) M = fmaxf(M, __ldcg(part(s) + D));
+  float M = -INFINITY, l = 0.f;
+  float2 o[PER];
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
-  if ((tid & 31) == 0) s_red[tid >> 5] = M;
-  __syncthreads();
-  for (int w = 0; w < D / 32; ++w) M = fmaxf(M, s_red[w]);
-  float o = 0.f, l = 0.f;
-  for (int s0 = 0; s0 < n_parts; s0 += 256) {
-    const int n = min(256, n_parts - s0);
-    __syncthreads();
-    for (int s = tid; s < n; s += D) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(s0 + s) + D));
-      s_w[s] = M == -INFINITY ? 0.f : exp2f(ml.x - M);
-      s_l[s] = ml.y;
-    }
-    __syncthreads();
+  for (int e = 0; e < PER; ++e) o[e] = make_float2(0.f, 0.f);
+  for (int s0 = 0; s0 < n_parts; s0 += 32) {           // 32 parts at a time
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (s0 + lane < n_parts) ml = __ldcg(reinterpret_cast<const float2*>(part(s0 + lane) + D));
+    float mx = ml.x;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+    const float to = fmaxf(M, mx), corr = M == to ? 1.f : exp2f(M - to);
+    M = to;
+    const float w = to == -INFINITY ? 0.f : exp2f(ml.x - to);
+    float add = w * ml.y;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) add += __shfl_xor_sync(0xffffffffu, add, off);
+    l = l * corr + add;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) { o[e].x *= corr; o[e].y *= corr; }
+    const int n = min(32, n_parts - s0);
 #pragma unroll 8
     for (int s = 0; s < n; ++s) {
-      o += s_w[s] * __ldcg(part(s0 + s) + tid);
-      l += s_w[s] * s_l[s];
+      const float ws = __shfl_sync(0xffffffffu, w, s);
+      const float2* p = reinterpret_cast<const float2*>(part(s0 + s));
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const float2 x = __ldcg(p + e * 32 + lane);
+        o[e].x += ws * x.x; o[e].y += ws * x.y;
+      }
     }
   }
-  const size_t rh = (size_t)(u.x + col / a.G) * a.Hq + u.y * a.G + col % a.G;
-  qt_store(a.out, a.out_type, rh * D + tid, l != 0.f ? o / l : 0.f);
+  const size_t rh = ((size_t)(u.x + col / a.G) * a.Hq + u.y * a.G + col % a.G) * D;
+  const float inv = l != 0.f ? 1.f / l : 0.f;          // (a NaN sum is not 0)
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const size_t i = rh + (e * 32 + lane) * 2;
+    if (a.out_type == GP_TYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + i) = make_float2(o[e].x * inv, o[e].y * inv);
+    else *reinterpret_cast<uint32_t*>(static_cast<unsigned short*>(a.out) + i) = qc_pack(o[e].x * inv, o[e].y * inv, a.out_type == GP_TYPE_F16);
+  }
 }
-

@@ -7,9 +7,10 @@ constexpr int QP_M = 128;                      // columns (row, query head of th
 constexpr int QP_COLS = 2 * QP_M;
 constexpr int QP_N = 64;                       // tokens of a step
 constexpr int QP_RING = 4;                     // steps whose keys and values there is room for
-constexpr int QP_SOFT = 256, QP_CONV = 128;    // threads that turn logits into weights, a column each; that turn codes into fp16
-constexpr int QP_THREADS = QP_SOFT + QP_CONV + 64;
-constexpr int QP_ISSUER = 12;                  // the first of the two warps that issue the products, one for each half
+constexpr int QP_SOFT = 256;                   // threads that turn logits into weights, a column each (warps 0 .. 7)
+constexpr int QP_TURN = 3;                     // warps that turn keys into fp16, a step each in turn (8 .. 10); as many turn values (11 .. 13)
+constexpr int QP_ISSUER = 14;                  // the first of the two warps that issue the products, one for each half
+constexpr int QP_THREADS = QP_SOFT + (2 * QP_TURN + 2) * 32;
 constexpr int QP_UNIT = 256;                   // what a unit costs beside its tokens, in tokens
 constexpr float QP_SLACK = 7.f;                // a row's maximum is brought up to date when something passes it by 2^7
 constexpr float QP_LIFT = 8.f;
@@ -47,7 +48,7 @@ __device__ __forceinline__ void qp_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void qp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void qp_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void qp_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 32 / 16 columns of the warp's 32 lanes
+// 32, 16, 8 columns of the warp's 32 lanes
 __device__ __forceinline__ void qp_ld32(uint32_t t, float* x) {
   uint32_t* r = reinterpret_cast<uint32_t*>(x);
   asm volatile(
@@ -56,6 +57,11 @@ __device__ __forceinline__ void qp_ld32(uint32_t t, float* x) {
         "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(t));
+}
+__device__ __forceinline__ void qp_st8(uint32_t t, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(t), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]),
+               "r"(r[7])
+               : "memory");
 }
 __device__ __forceinline__ void qp_ld16(uint32_t t, float* x) {
   uint32_t* r = reinterpret_cast<uint32_t*>(x);
@@ -72,13 +78,13 @@ __device__ __forceinline__ void qp_st16(uint32_t t, const uint32_t* r) {
 
 struct QpShared {
   // [half], and by the place of the step in its ring
-  uint64_t q_full[2], k_full[QP_RING], v_full[QP_RING], s_full[2][QP_RING], p_full[2][2], o_full[2][QP_RING], sc_full[2 * QP_RING];
+  uint64_t q_full[2], k_full[QP_RING], v_full[QP_RING], k_free[QP_RING], v_free[QP_RING], s_full[2][QP_RING], p_full[2][2], o_full[2][QP_RING];
   uint32_t tmem;
   int dead;                                    // a wait ran out: all others end at once
   int nan[8];                                  // by the number of the piece: that number, where a value is no number and rows see different tokens
   alignas(16) float ks[2 * QP_RING][QP_N / 16], ev[2 * QP_RING][QP_N / 16];      // per group of 16 tokens: scale of the keys (-1: no such page), exponent of that of the values
   long long x1, share, upto[QP_THREADS], warp[QP_THREADS / 32];
-  float plain[2][QT_WARPS * 130];
+  float plain[2][QT_WARPS * 130], qs[2][QP_M];
 };
 // A bounded wait for a phase of a barrier.
 __device__ __forceinline__ void qp_wait(QpShared& sh, uint64_t* bar, uint32_t parity) {
@@ -185,7 +191,7 @@ struct QpWalk {
 //   S [128 columns x 64 tokens] = Q K^T       (tcgen05, fp16 in shared memory, S in tensor memory)
 //   P = weights of S                           (four warps, a thread a column; fp16, over S in tensor memory)
 //   O [128 columns x d] += P V                 (tcgen05, P from tensor memory, V in shared memory)
-// There are two S of each half, so that the logits of the next step are there when the weights of one are done.  Four more warps bring codes in and
+// There are two S of each half, so that the logits of the next step are there when the weights of one are done.  Six more warps bring codes in and
 // write them to shared memory as fp16, which holds them exactly and unscaled: K and V in the same image (a token's channels along a row, 64 a
 // swizzled 128 bytes), which the first product reads with the channels, the second with the tokens as inner dimension; four steps of them are there.
 // A warp more for each half issues its products.
@@ -212,10 +218,10 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     for (int h = 0; h < 2; ++h) {
       mbar_init(&sh.q_full[h], 4);
       for (int i = 0; i < 2; ++i) mbar_init(&sh.p_full[h][i], 4);
-      for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.s_full[h][i], 1); mbar_init(&sh.o_full[h][i], 1); }
+      for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.s_full[h][i], 2); mbar_init(&sh.o_full[h][i], 1); }
     }
-    for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.k_full[i], 4); mbar_init(&sh.v_full[i], 4); }
-    for (int i = 0; i < 2 * QP_RING; ++i) { mbar_init(&sh.sc_full[i], 1); sh.nan[i] = -1; }
+    for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.v_full[i], 1); mbar_init(&sh.k_free[i], 2); mbar_init(&sh.v_free[i], 2); }
+    for (int i = 0; i < 8; ++i) sh.nan[i] = -1;
     sh.dead = 0;
     fence_mbar_init();
     a.joins[blockIdx.x * 2] = make_int4(0, 0, 0, 0);
@@ -238,7 +244,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     const uint32_t idesc = 1u << 4 | (QP_M / 16u) << 24, qk = idesc | (QP_N / 8u) << 17, pv = idesc | 1u << 16 | (D / 8u) << 17;
     const uint32_t half = __shfl_sync(0xffffffffu, (uint32_t)(warp - QP_ISSUER), 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t dq = qp_desc(q_smem + half * QOPERAND, 16), dk = qp_desc(k_smem, 16), dv = qp_desc(v_smem, QP_BLOCK);
-    const uint32_t t_s = tm + T_S + half * 128, t_o = tm + T_O + half * 128, s_full = smem_u32(&sh.s_full[half][0]), o_full = smem_u32(&sh.o_full[half][0]);
+    const uint32_t t_s = tm + T_S + half * 128, t_o = tm + T_O + half * 128, s_full = smem_u32(&sh.s_full[half][0]), o_full = smem_u32(&sh.o_full[half][0]),
+                   k_free = smem_u32(sh.k_free), v_free = smem_u32(sh.v_free);
     int4 join[2];
     join[0].x = 0;
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
@@ -257,6 +264,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
               qp_mma_ss(t_s + (s & 1) * 64, dq + (((k >> 2) * QP_QBLOCK + (k & 3) * 32) >> 4), k0 + (((k >> 2) * QP_BLOCK + (k & 3) * 32) >> 4), qk, k > 0);
           }
           qp_commit(s_full + (s & (QP_RING - 1)) * 8);
+          if (lane == 0) qp_arrive(&sh.s_full[half][s & (QP_RING - 1)]);      // hands on what it saw of the step: its scales
+          qp_commit(k_free + (s & (QP_RING - 1)) * 8);
         }
         if (j > 0) {
           const uint32_t b = s - 1;
@@ -272,102 +281,93 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
                 qp_mma_ts(t_o, t_s + (b & 1) * 64 + t * 32 + k * 8, v0 + k * (2048 >> 4), pv, t > 0 || k > 0 ? 1u : (uint32_t)(j > 1));
           }
           qp_commit(o_full + (b & (QP_RING - 1)) * 8);
+          qp_commit(v_free + (b & (QP_RING - 1)) * 8);
         }
       }
       n += p.n_steps;
     }
     if (warp == QP_ISSUER && lane == 0 && join[0].x > 0) { a.joins[blockIdx.x * 2] = join[0]; a.joins[blockIdx.x * 2 + 1] = join[1]; }
-  } else if (warp >= 8) {                               // ---- codes to fp16
-    const int ct = tid - QP_SOFT, cw = warp - 8;
-    constexpr int TPI = QP_CONV / CH;                   // tokens of a round, a multiple of 8
+  } else if (warp >= 8) {                               // ---- codes to fp16: three warps the keys, three the values, a step each in turn
+    const int kv = (warp - 8) / QP_TURN, turn = (warp - 8) % QP_TURN;
+    constexpr int TPI = 32 / CH;                        // tokens of a round: 4 or 8
     constexpr int IT = QP_N / TPI;
-    const int ch = ct % CH, tt = ct / CH;               // piece of 16 channels; token in the round
+    const int ch = lane % CH, tt = lane / CH;           // piece of 16 channels; token in the round
     // its place in a row of 128 bytes, swizzled; the two halves of 128 channels write their two pieces in opposite order: no bank twice
     const int flip = (ch >> 2) & 1;
-    const uint32_t dst = (ch >> 2) * QP_BLOCK + tt * 128, at0 = ((((ch & 3) * 2 + flip) ^ (tt & 7)) << 4), at1 = at0 ^ 16;
+    const uint32_t dst = (kv ? v_smem : k_smem) + (ch >> 2) * QP_BLOCK + tt * 128, at0 = ((((ch & 3) * 2 + flip) ^ (tt & 7)) << 4), at1 = at0 ^ 16;
     const size_t page_bytes = (size_t)c.Hkv * 2 * c.page * D;
+    const uint32_t full = smem_u32(kv ? sh.v_full : sh.k_full);
+    uint64_t* empty = kv ? sh.v_free : sh.k_free;       // both halves' products have read what was there
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       const QtUnit& u = p.u;
       const int vis0 = qt_visible(c, u, a.G, 0);        // of the first row: the least
-      const uint8_t* head = c.codes + (size_t)u.h * 2 * c.page * D + ch * 16;
-      // lanes 0 .. 3: page of a group of 16 tokens of a step
+      const uint8_t* src = c.codes + (size_t)(u.h * 2 + kv) * c.page * D + ch * 16;
+      const int* table = c.table + (size_t)u.seq * c.stride;
+      // lanes 0 .. 3: page of a group of 16 tokens of a step, as the table has it (looked at a turn later: nothing waits for it here)
       auto page_of = [&](int j) {
         const int t = u.t0 + j * QP_N + lane * 16;
-        return lane < QP_N / 16 && t < u.t1 ? qc_page(c, u.seq, t >> c.page_log) : -1;
+        return lane < QP_N / 16 && t < u.t1 ? table[t >> c.page_log] : -1;
       };
-      auto load = [&](uint4* r, int j, int ids, int kv) {
+      uint4 r[IT];
+      float2 sc;
+      auto load = [&](int j, int ids) {
         const int first = u.t0 + j * QP_N;
-        const uint8_t* src = head + (size_t)kv * c.page * D;
+        if ((unsigned)ids >= (unsigned)c.n_pages) {
+          if (lane < QP_N / 16 && first + lane * 16 < u.t1 && c.status) atomicOr(c.status, GP_E_BOUNDS);
+          ids = -1;
+        }
         const bool all = first + QP_N <= u.t1 && __all_sync(0xffffffffu, ids >= 0 || lane >= QP_N / 16);
+        const int slot0 = first & (c.page - 1);
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
           const int t = i * TPI + tt;
-          const int id = __shfl_sync(0xffffffffu, ids, t >> 4);
-          const uint4* from = reinterpret_cast<const uint4*>(src + (size_t)max(id, 0) * page_bytes + ((first + t) & (c.page - 1)) * D);
-          if (all) r[i] = __ldg(from);
-          else r[i] = id >= 0 && first + t < u.t1 ? __ldg(from) : make_uint4(0, 0, 0, 0);
+          const int id = __shfl_sync(0xffffffffu, ids, i * TPI / 16);
+          const uint4* from = reinterpret_cast<const uint4*>(src + (size_t)max(id, 0) * page_bytes + ((slot0 + t) & (c.page - 1)) * D);
+          r[i] = all || (id >= 0 && first + t < u.t1) ? __ldg(from) : make_uint4(0, 0, 0, 0);
         }
+        sc = make_float2(-1.f, 1.f);
+        if (!kv && ids >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((size_t)ids * c.Hkv + u.h) * 2);
       };
-      auto store = [&](const uint4* r, uint32_t to) {
+      const int j0 = (turn + QP_TURN - n % QP_TURN) % QP_TURN;      // its first step of the piece
+      int next = 0;
+      if (j0 < p.n_steps) {
+        load(j0, page_of(j0));
+        next = page_of(j0 + QP_TURN);
+      }
+      for (int j = j0; j < p.n_steps; j += QP_TURN) {
+        const int s = n + j;
+        const int at = s & (QP_RING - 1);
+        if (s >= QP_RING) qp_wait(sh, empty + at, ((s - QP_RING) / QP_RING) & 1);
+        if (!kv) {
+          const int slot = s & (2 * QP_RING - 1);       // (twice the ring: the weights of a step may still be computed when its keys are replaced)
+          if (lane < QP_N / 16) { sh.ks[slot][lane] = sc.x; sh.ev[slot][lane] = (float)((int)((__float_as_uint(sc.y) >> 23) & 255) - 127); }
+        } else if (u.t0 + (j + 1) * QP_N > vis0) {      // rows see different tokens of the step
+          bool nan = false;
+#pragma unroll
+          for (int i = 0; i < IT; ++i)
+            nan |= (__vcmpeq4(r[i].x & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(r[i].y & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(r[i].z & 0x7f7f7f7f, 0x7f7f7f7f) |
+                    __vcmpeq4(r[i].w & 0x7f7f7f7f, 0x7f7f7f7f)) != 0;
+          if (nan) *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) = piece;
+        }
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-          const uint32_t x0 = flip ? r[i].z : r[i].x, y0 = flip ? r[i].w : r[i].y, x1 = flip ? r[i].x : r[i].z, y1 = flip ? r[i].y : r[i].w;
-          const uint32_t row = to + dst + i * TPI * 128;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + at0), "r"(e4m3x2_to_f16x2(x0)), "r"(e4m3x2_hi_to_f16x2(x0)), "r"(e4m3x2_to_f16x2(y0)),
-                       "r"(e4m3x2_hi_to_f16x2(y0))
+          const uint32_t xa = flip ? r[i].z : r[i].x, ya = flip ? r[i].w : r[i].y, xb = flip ? r[i].x : r[i].z, yb = flip ? r[i].y : r[i].w;
+          const uint32_t row = dst + at * OPERAND + i * TPI * 128, odd = TPI == 4 ? (i & 1) << 6 : 0;      // (token & 7 goes by the round too)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (at0 ^ odd)), "r"(e4m3x2_to_f16x2(xa)), "r"(e4m3x2_hi_to_f16x2(xa)),
+                       "r"(e4m3x2_to_f16x2(ya)), "r"(e4m3x2_hi_to_f16x2(ya))
                        : "memory");
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + at1), "r"(e4m3x2_to_f16x2(x1)), "r"(e4m3x2_hi_to_f16x2(x1)), "r"(e4m3x2_to_f16x2(y1)),
-                       "r"(e4m3x2_hi_to_f16x2(y1))
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (at1 ^ odd)), "r"(e4m3x2_to_f16x2(xb)), "r"(e4m3x2_hi_to_f16x2(xb)),
+                       "r"(e4m3x2_to_f16x2(yb)), "r"(e4m3x2_hi_to_f16x2(yb))
                        : "memory");
         }
         fence_proxy_async();
         __syncwarp();
-      };
-      auto scales_of = [&](int ids) {
-        float2 sc = make_float2(-1.f, 1.f);
-        if (cw == 0 && ids >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((size_t)ids * c.Hkv + u.h) * 2);
-        return sc;
-      };
-      uint4 kr[IT], vr[IT];
-      int ids = page_of(0), ids1 = page_of(1);
-      load(kr, 0, ids, 0);
-      load(vr, 0, ids, 1);
-      float2 sc = scales_of(ids);
-      for (int j = 0; j < p.n_steps; ++j) {
-        const int s = n + j;
-        const int ids2 = page_of(j + 2);
-        const int at = s & (QP_RING - 1), before = ((s - QP_RING) / QP_RING) & 1;
-        if (s >= QP_RING) {                             // both halves' products have read the keys that were here
-          qp_wait(sh, &sh.s_full[0][at], before);
-          qp_wait(sh, &sh.s_full[1][at], before);
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
+        if (j + QP_TURN < p.n_steps) {
+          load(j + QP_TURN, next);
+          next = page_of(j + 2 * QP_TURN);
         }
-        if (cw == 0) {
-          const int slot = s & (2 * QP_RING - 1);       // (twice the ring: the weights of a step may still be computed when its keys are replaced)
-          if (lane < QP_N / 16) { sh.ks[slot][lane] = sc.x; sh.ev[slot][lane] = (float)((int)((__float_as_uint(sc.y) >> 23) & 255) - 127); }
-          __syncwarp();
-          if (lane == 0) qp_arrive(&sh.sc_full[slot]);
-        }
-        store(kr, k_smem + at * OPERAND);
-        if (lane == 0) qp_arrive(&sh.k_full[at]);
-        load(kr, j + 1, ids1, 0);
-        sc = scales_of(ids1);
-        if (u.t0 + (j + 1) * QP_N > vis0) {             // rows see different tokens of the step
-          bool nan = false;
-#pragma unroll
-          for (int i = 0; i < IT; ++i)
-            nan |= (__vcmpeq4(vr[i].x & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(vr[i].y & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(vr[i].z & 0x7f7f7f7f, 0x7f7f7f7f) |
-                    __vcmpeq4(vr[i].w & 0x7f7f7f7f, 0x7f7f7f7f)) != 0;
-          if (nan) *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) = piece;
-        }
-        if (s >= QP_RING) {
-          qp_wait(sh, &sh.o_full[0][at], before);
-          qp_wait(sh, &sh.o_full[1][at], before);
-        }
-        store(vr, v_smem + at * OPERAND);
-        if (lane == 0) qp_arrive(&sh.v_full[at]);
-        load(vr, j + 1, ids1, 1);
-        ids1 = ids2;
       }
       n += p.n_steps;
     }
@@ -382,33 +382,45 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       u.rows = max(min(RT, u.rows - half * RT), 0);
       u.cols = u.rows * a.G;
       const bool used = u.cols > 0, real = t128 < u.cols;
-      const int my = min(t128, max(u.cols - 1, 0));
-      const int row = u.row0 + my / a.G, head = u.h * a.G + my % a.G;
       const int see = real ? qt_visible(c, u, a.G, t128) : 0x7fffffff;
       float qs = 0.f;                                   // what S is multiplied with
-      if (used && p.n_steps > 0) {
-        const unsigned short* src = a.q + (size_t)row * a.q_stride + (size_t)head * D;
-        float mx = 0.f;
+      if (used && p.n_steps > 0) {                      // the warp's 32 columns, D / 8 lanes a column
+        constexpr int LPC = D / 8, CPR = 32 / LPC, ROUNDS = 32 / CPR;
+        const int piece8 = lane % LPC;
+        // (code that runs once a unit is kept short: its instructions come from far away every time)
+#pragma unroll 1
+        for (int i0 = 0; i0 < ROUNDS; i0 += 4) {
+          uint4 w[4];
+          int col0 = (warp & 3) * 32 + i0 * CPR + lane / LPC;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 w = *reinterpret_cast<const uint4*>(src + i * 8);
-          for (uint32_t e : {w.x, w.y, w.z, w.w}) { const float2 x = qc_elems(e, a.f16); mx = fmaxf(mx, fmaxf(fabsf(x.x), fabsf(x.y))); }
-        }
-        const int ex = max((int)(__float_as_uint(mx) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
-        const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
-        qs = 1.4426950408889634f * rsqrtf((float)D) * __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          uint4 w = *reinterpret_cast<const uint4*>(src + i * 8);
-          for (uint32_t* e : {&w.x, &w.y, &w.z, &w.w}) {
-            const float2 x = qc_elems(*e, a.f16);
-            const __half2 h = __floats2half2_rn(real ? x.x * mul : 0.f, real ? x.y * mul : 0.f);
-            *e = *reinterpret_cast<const uint32_t*>(&h);
+          for (int i = 0; i < 4; ++i) {
+            const int col = col0 + i * CPR;
+            w[i] = make_uint4(0, 0, 0, 0);
+            if (col < u.cols) w[i] = *reinterpret_cast<const uint4*>(a.q + (size_t)(u.row0 + col / a.G) * a.q_stride + (size_t)(u.h * a.G + col % a.G) * D + piece8 * 8);
           }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + half * QOPERAND + (i >> 3) * QP_QBLOCK + t128 * 128 + (((i & 7) ^ (t128 & 7)) << 4)),
-                       "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
-                       : "memory");
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int col = col0 + i * CPR;
+            float mx = 0.f;
+            for (uint32_t e : {w[i].x, w[i].y, w[i].z, w[i].w}) { const float2 x = qc_elems(e, a.f16); mx = fmaxf(mx, fmaxf(fabsf(x.x), fabsf(x.y))); }
+#pragma unroll
+            for (int o = 1; o < LPC; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const int ex = max((int)(__float_as_uint(mx) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
+            const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
+            const float down = 1.4426950408889634f * rsqrtf((float)D) * __uint_as_float((uint32_t)(127 - up) << 23);
+            if (piece8 == 0) sh.qs[half][col & 127] = down;
+            for (uint32_t* e : {&w[i].x, &w[i].y, &w[i].z, &w[i].w}) {
+              const float2 x = qc_elems(*e, a.f16);
+              const __half2 h = __floats2half2_rn(x.x * mul, x.y * mul);
+              *e = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + half * QOPERAND + (piece8 >> 3) * QP_QBLOCK + col * 128 + (((piece8 & 7) ^ (col & 7)) << 4)),
+                         "r"(w[i].x), "r"(w[i].y), "r"(w[i].z), "r"(w[i].w)
+                         : "memory");
+          }
         }
+        __syncwarp();
+        qs = sh.qs[half][t128];
         fence_proxy_async();
       }
       __syncwarp();
@@ -418,7 +430,6 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       for (int j = 0; j < p.n_steps; ++j) {
         const int s = n + j;
         const int slot = s & (2 * QP_RING - 1);
-        qp_wait(sh, &sh.sc_full[slot], (s / (2 * QP_RING)) & 1);
         qp_wait(sh, &sh.s_full[half][s & (QP_RING - 1)], (s / QP_RING) & 1);
         qp_fence_after();
         if (used) {
@@ -447,14 +458,15 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             }
           }
           float mx = -INFINITY;                         // the largest s + ev of the step
-          auto top_of = [&](const float* x, int g) {    // of 16 columns
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const float* x = (g & 2 ? x1 : x0) + (g & 1) * 16;
             float m0 = qp_max3(x[0], x[1], x[2]), m1 = qp_max3(x[3], x[4], x[5]);
             m0 = qp_max3(m0, x[6], x[7]); m1 = qp_max3(m1, x[8], x[9]);
             m0 = qp_max3(m0, x[10], x[11]); m1 = qp_max3(m1, x[12], x[13]);
             m0 = qp_max3(m0, x[14], x[15]);
             mx = fmaxf(mx, fmaf(fmaxf(m0, m1), f[g], ev[g]));
-          };
-          top_of(x0, 0); top_of(x0 + 16, 1); top_of(x1, 2); top_of(x1 + 16, 3);
+          }
           // maximum and E
           float dE = 0.f;
           if (top > -1000.f) {
@@ -487,37 +499,32 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             }
           }
           const float zero = M == -INFINITY ? 0.f : M;
-          auto weigh = [&](const float* x, int at) {    // weights of 32 columns to tensor memory
-            uint32_t hi[16], lo[16];
 #pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-              const int g = at / 16 + hf;
-              const float b1 = ev[g] - zero;
-              const uint64_t ff = qp_pack2(f[g], f[g]), b = qp_pack2(b1, b1);
-              uint64_t sum = 0;
+          for (int g = 0; g < 4; ++g) {                 // weights of 16 columns to tensor memory
+            const float* x = (g & 2 ? x1 : x0) + (g & 1) * 16;
+            const uint64_t ff = qp_pack2(f[g], f[g]), b = qp_pack2(ev[g] - zero, ev[g] - zero);
+            uint64_t acc = 0;
+            uint32_t hi[8], lo[8];
 #pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                float p0, p1;
-                qp_unpack2(qp_fma2(qp_pack2(x[hf * 16 + e], x[hf * 16 + e + 1]), ff, b), p0, p1);
-                p0 = qt_exp2(p0); p1 = qt_exp2(p1);
-                sum = qp_add2(sum, qp_pack2(p0, p1));
-                const __half2 h = __floats2half2_rn(p0, p1);
-                hi[hf * 8 + e / 2] = *reinterpret_cast<const uint32_t*>(&h);
-                if (TERMS == 2) {
-                  const float2 b2 = __half22float2(h);
-                  const __half2 r = __floats2half2_rn(p0 - b2.x, p1 - b2.y);
-                  lo[hf * 8 + e / 2] = *reinterpret_cast<const uint32_t*>(&r);
-                }
+            for (int e = 0; e < 16; e += 2) {
+              float p0, p1;
+              qp_unpack2(qp_fma2(qp_pack2(x[e], x[e + 1]), ff, b), p0, p1);
+              p0 = qt_exp2(p0); p1 = qt_exp2(p1);
+              acc = qp_add2(acc, qp_pack2(p0, p1));
+              const __half2 h = __floats2half2_rn(p0, p1);
+              hi[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+              if (TERMS == 2) {
+                const float2 b2 = __half22float2(h);
+                const __half2 r = __floats2half2_rn(p0 - b2.x, p1 - b2.y);
+                lo[e / 2] = *reinterpret_cast<const uint32_t*>(&r);
               }
-              float s0, s1;
-              qp_unpack2(sum, s0, s1);
-              L = fmaf(s0 + s1, qt_exp2(fminf(E - ev[g], 100.f)), L);
             }
-            qp_st16(t_x + at / 2, hi);
-            if (TERMS == 2) qp_st16(t_x + 32 + at / 2, lo);
-          };
-          weigh(x0, 0);
-          weigh(x1, 32);
+            float s0, s1;
+            qp_unpack2(acc, s0, s1);
+            L = fmaf(s0 + s1, qt_exp2(fminf(E - ev[g], 100.f)), L);
+            qp_st8(t_x + g * 8, hi);
+            if (TERMS == 2) qp_st8(t_x + 32 + g * 8, lo);
+          }
           qp_wait_st();
         }
         qp_fence_before();
@@ -533,37 +540,62 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       // out = 2^E O / L; a part of a result: 2^E O, M - E, L
       const float scale = exp2f(E), inv = L != 0.f ? scale / L : 0.f;      // (a NaN sum is not 0)
       float* parts = p.whole ? nullptr : a.part + (size_t)(blockIdx.x * 2 + (p.begins ? 0 : 1)) * QP_COLS * ST + (size_t)half * RT * a.G * ST;
-      const size_t rh = ((size_t)row * a.Hq + head) * D;
-      float* part = parts + (size_t)t128 * ST;
+      // by way of the memory of the warp's own 32 queries (no product reads them any more), so that lanes store what lies together
+      const uint32_t stage = q_smem + half * QOPERAND + (warp & 3) * (32 * 128);
+      auto place = [&](int col, int pc) { return stage + (pc >> 3) * QP_QBLOCK + col * 128 + (((pc & 7) ^ (col & 7)) << 4); };
+      constexpr int PIECES = D / 8;                     // of 16 bytes, of a column there
+      const bool wide = parts || a.out_type == GP_TYPE_F32;      // two rounds of half of the channels in 32 bits, else one of all in 16
+      const float by = parts ? scale : inv;
 #pragma unroll 1
-      for (int g = 0; g < D / 32; ++g) {
-        float o[32];
+      for (int round = 0; round < (wide ? 2 : 1); ++round) {
+        const int chans = wide ? D / 2 : D;
+#pragma unroll 1
+        for (int g = 0; g < chans / 16; ++g) {
+          float o[16];
+          __syncwarp();
+          if (p.n_steps > 0) {
+            qp_ld16(t_o + round * (D / 2) + g * 16, o);
+            qp_wait_ld();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] *= by;
+          if (wide) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place(lane, g * 4 + e)), "f"(o[4 * e]), "f"(o[4 * e + 1]),
+                           "f"(o[4 * e + 2]), "f"(o[4 * e + 3])
+                           : "memory");
+          } else {
+            const bool f16 = a.out_type == GP_TYPE_F16;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place(lane, g * 2 + e)), "r"(qc_pack(o[8 * e], o[8 * e + 1], f16)),
+                           "r"(qc_pack(o[8 * e + 2], o[8 * e + 3], f16)), "r"(qc_pack(o[8 * e + 4], o[8 * e + 5], f16)), "r"(qc_pack(o[8 * e + 6], o[8 * e + 7], f16))
+                           : "memory");
+          }
+        }
         __syncwarp();
-        if (p.n_steps > 0) {
-          qp_ld32(t_o + g * 32, o);
-          qp_wait_ld();
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+#pragma unroll 2
+        for (int i = 0; i < PIECES; ++i) {              // 32 pieces a time
+          const int col = i * (32 / PIECES) + lane / PIECES, pc = lane % PIECES, cc = (warp & 3) * 32 + col;
+          uint4 w;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place(col, pc)));
+          if (cc >= u.cols) continue;
+          if (parts) {
+            float2* to = reinterpret_cast<float2*>(parts + (size_t)cc * ST + round * (D / 2) + pc * 4);
+            to[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+            to[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+          } else {
+            uint8_t* to = static_cast<uint8_t*>(a.out) + ((size_t)(u.row0 + cc / a.G) * a.Hq + u.h * a.G + cc % a.G) * D * (wide ? 4 : 2);
+            *reinterpret_cast<uint4*>(to + round * (2 * D) + pc * 16) = w;
+          }
         }
-        if (!real) {
-        } else if (parts) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) *reinterpret_cast<float2*>(part + g * 32 + e) = make_float2(o[e] * scale, o[e + 1] * scale);
-        } else if (a.out_type == GP_TYPE_F32) {
-          float4* dst = reinterpret_cast<float4*>(static_cast<float*>(a.out) + rh + g * 32);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e] * inv, o[4 * e + 1] * inv, o[4 * e + 2] * inv, o[4 * e + 3] * inv);
-        } else {
-          const bool f16 = a.out_type == GP_TYPE_F16;
-          uint4* dst = reinterpret_cast<uint4*>(static_cast<unsigned short*>(a.out) + rh + g * 32);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(qc_pack(o[8 * e] * inv, o[8 * e + 1] * inv, f16), qc_pack(o[8 * e + 2] * inv, o[8 * e + 3] * inv, f16),
-                                qc_pack(o[8 * e + 4] * inv, o[8 * e + 5] * inv, f16), qc_pack(o[8 * e + 6] * inv, o[8 * e + 7] * inv, f16));
-        }
+        __syncwarp();
       }
-      if (parts && real) { part[D] = M == -INFINITY ? M : M - E; part[D + 1] = L; }
+      if (parts && real) { parts[(size_t)t128 * ST + D] = M == -INFINITY ? M : M - E; parts[(size_t)t128 * ST + D + 1] = L; }
       if (p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece)      // some row may have met another's NaN: all of the half in plain arithmetic
         qt_plain<D>(c, a, u, sh.plain[half], parts, 1 + half);
     }
@@ -583,7 +615,7 @@ int qp_run(const QcDev& c, const QtArgs& a, const QpPlan& p, cudaStream_t s) {
   const size_t smem = (D / 64) * (2 * QP_QBLOCK + 2 * QP_RING * QP_BLOCK) + 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
   if (gp_launch(kern, p.blocks, QP_THREADS, smem, s, false, c, a) != cudaSuccess) return GP_ERR_CUDA;
-  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, QP_COLS, 2>, p.blocks * QP_COLS, D, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
+  if (p.blocks > 1 && gp_launch(qt_merge_kernel<D, QP_COLS, 2>, p.blocks * (QP_COLS / 4), 128, 0, s, true, a) != cudaSuccess) return GP_ERR_CUDA;
   return GP_OK;
 }
 
