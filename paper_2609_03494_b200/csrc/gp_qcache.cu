@@ -17,121 +17,170 @@ struct QcFreq { double over_pi[64]; };      // theta^(-2i/d) / pi: angles in uni
 
 constexpr int QA_THREADS = 256;
 constexpr int QA_WARPS = QA_THREADS / 32;
+constexpr int QA_QROWS = 16;                   // rows whose queries a block takes
 
-// least e with amax <= 448 * 2^e = 0.875 * 2^(e + 9)
-__device__ __forceinline__ int qc_exponent(double amax) {
-  if (!(amax > 0.0)) return QC_E_MIN;
-  int x;
-  const double f = frexp(amax, &x);
-  return min(max(x - 9 + (f > 0.875 ? 1 : 0), QC_E_MIN), QC_E_MAX);
+// A magnitude as an integer of the same order, as far as the exponent of a scale needs it: the high word of the double and whether anything follows
+// (32 bits take one instruction to reduce over a warp).
+__device__ __forceinline__ uint32_t qc_size(double x) { return (uint32_t)__double2hiint(x) * 2u + min((uint32_t)__double2loint(x), 1u); }
+constexpr uint32_t QC_FAR64 = (1023u + 127u) << 21;             // size of 2^127: from here on fp32 may not hold the number
+// the same of two 16-bit numbers in one register; QC_INF16: sizes that are not finite begin here
+__device__ __forceinline__ uint32_t qc_sizes(uint32_t two) { return two & 0x7fff7fffu; }
+template <bool F16> constexpr uint32_t QC_INF16 = F16 ? 0x7c00u : 0x7f80u;
+// least e with amax <= 448 * 2^e = 0.875 * 2^(e + 9), from the exponent field over its bias and whether the mantissa is above 1.75
+__device__ __forceinline__ int qc_exponent(uint32_t size, int exponent, bool above) {
+  return size == 0 ? QC_E_MIN : min(max(exponent - 8 + (above ? 1 : 0), QC_E_MIN), QC_E_MAX);
 }
+__device__ __forceinline__ int qc_exponent64(uint32_t size) { return qc_exponent(size, (int)(size >> 21) - 1023, (size & 0x1fffff) > 0x180000); }
+__device__ __forceinline__ int qc_exponent32(uint32_t size) { return qc_exponent(size, (int)(size >> 23) - 127, (size & 0x7fffff) > 0x600000); }
 __device__ __forceinline__ int qc_scale_exponent(float s) {      // of a scale that is there; anything else is brought into the range
   return min(max((int)((__float_as_uint(s) >> 23) & 255) - 127, QC_E_MIN), QC_E_MAX);
 }
 __device__ __forceinline__ float pow2f(int e) {                  // 2^e, 0 below the normal numbers
   return e < -126 ? 0.f : __uint_as_float((uint32_t)(e + 127) << 23);
 }
+// 1 / sqrt(x) in fp64: Newton's iteration on y^-2 - x from the fp32 result, twice (2^-22, 2^-44, beyond fp64)
+__device__ __forceinline__ double qc_rsqrt(double x) {
+  const float f = (float)x;
+  if (!(f > 1e-30f && f < 1e30f)) return 1.0 / sqrt(x);
+  double y = rsqrtf(f);
+  y = y * fma(-0.5 * x * y, y, 1.5);
+  return y * fma(-0.5 * x * y, y, 1.5);
+}
+// eight 16-bit elements, two at a time
+template <bool F16>
+__device__ __forceinline__ void qc_elems8(const uint4& w, float* x) {
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) { const float2 t = qc_elems(v[e], F16); x[2 * e] = t.x; x[2 * e + 1] = t.y; }
+}
+// two fp32 numbers at a time
+__device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// four numbers to e4m3, known to be finite
+__device__ __forceinline__ uint32_t qc_codes_finite(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
 
-// A team of TEAM warps takes one (page, KV head) at a time, keys first, then values: a row lies in D / 8 lanes (four elements of
-// its first half and four of its second, so that a lane has both elements of the pairs it rotates), a team takes TEAM * 256 / D rows in a
-// pass and keeps up to PASSES passes in registers until the largest magnitude of all of them is known.  The angles of the block's tokens
-// are computed once for all heads (TABLE), in fp64, as the keys are: their largest magnitude decides an integer, and against a definition
-// in 64 bits only 64 bits decide it alike.  Values need no arithmetic before their maximum.
-// Queries (the last blocks of the grid) decide nothing: fp32, with angles reduced in fp64.
-template <int D, int TEAM, int PASSES, bool TABLE>
-__global__ void __launch_bounds__(QA_THREADS)
-qc_append_kernel(const QcDev c, const QcRows r, const __grid_constant__ QcFreq freq, int places, int groups, int heads_per, int kv_blocks,
-                 int q_rows) {
-  constexpr int LPR = D / 8;                          // lanes per row
+// Queries of up to 16 rows of a sequence, for a part of the heads.
+template <int D, bool F16>
+__device__ __forceinline__ void qc_append_queries(const QcDev& c, const QcRows& r, const QcFreq& freq, int at, int places, int groups, int heads_per, float2* tab) {
+  constexpr int LPR = D / 16, RPW = 32 / LPR, HALF = D / 2;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane % LPR, sub = lane / LPR;
+  const int q0 = at % groups * heads_per, q1 = min(q0 + heads_per, r.Hq); at /= groups;
+  const int place = at % places, s = at / places;
+  const QcSeq q = qc_seq(c, s);
+  const int i0 = max(place * QA_QROWS, -q.slot0), i1 = min(min((place + 1) * QA_QROWS, q.rows), c.limit - q.slot0);      // rows that lie in a slot
+  const int nt = i1 - i0;
+  if (nt <= 0) return;
+  const int row0 = q.r0 + i0, slot = q.slot0 + i0;
+  if (r.rope) {
+    for (int i = tid; i < nt * HALF; i += QA_THREADS) {
+      const int t = i / HALF;
+      const double g = (r.positions ? r.positions[row0 + t] : slot + t) * freq.over_pi[i % HALF];
+      float sn, cs;
+      sincospif((float)(g - 2.0 * rint(0.5 * g)), &sn, &cs);
+      tab[t * HALF + i % 8 * LPR + i % HALF / 8] = make_float2(cs, sn);
+    }
+    __syncthreads();
+  }
+  const int per = max(1, QA_WARPS / nt);              // warps a token has
+  float w0[8], w1[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { w0[e] = r.qw ? r.qw[lr * 8 + e] : 1.f; w1[e] = r.qw ? r.qw[HALF + lr * 8 + e] : 1.f; }
+  for (int t = warp / per; t < nt; t += QA_WARPS / per) {
+    uint64_t ca[4], sa[4], cb[4], sb[4];              // first half = inv (ca x + sa y), second = inv (cb y + sb x), two at a time
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float2 i = make_float2(1.f, 0.f), j = i;
+      if (r.rope) { i = tab[t * HALF + 2 * e * LPR + lr]; j = tab[t * HALF + (2 * e + 1) * LPR + lr]; }
+      ca[e] = pack2(w0[2 * e] * i.x, w0[2 * e + 1] * j.x);
+      sa[e] = pack2(-w1[2 * e] * i.y, -w1[2 * e + 1] * j.y);
+      cb[e] = pack2(w1[2 * e] * i.x, w1[2 * e + 1] * j.x);
+      sb[e] = pack2(w0[2 * e] * i.y, w0[2 * e + 1] * j.y);
+    }
+    const unsigned short* src = r.q + (size_t)(row0 + t) * r.q_stride + lr * 8;
+    unsigned short* dst = r.q_out + (size_t)(row0 + t) * r.qo_stride + lr * 8;
+    auto load = [&](int h, uint4* w) {
+      w[0] = w[1] = make_uint4(0, 0, 0, 0);
+      if (h < q1) {
+        w[0] = *reinterpret_cast<const uint4*>(src + h * D);
+        w[1] = *reinterpret_cast<const uint4*>(src + h * D + HALF);
+      }
+    };
+    int h = q0 + warp % per * RPW + sub;
+    uint4 now[2], then[2];
+    load(h, now);
+    for (; h - sub < q1; h += per * RPW) {
+      load(h + per * RPW, then);
+      float x[8], y[8], inv = 1.f;
+      qc_elems8<F16>(now[0], x);
+      qc_elems8<F16>(now[1], y);
+      if (r.qw) {
+        uint64_t ss = 0;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const uint64_t xx = pack2(x[e], x[e + 1]), yy = pack2(y[e], y[e + 1]);
+          ss = fma2(xx, xx, ss);
+          ss = fma2(yy, yy, ss);
+        }
+        float s0, s1;
+        unpack2(ss, s0, s1);
+        s0 += s1;
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+        inv = 1.f / sqrtf(s0 * (1.f / D) + (float)r.eps);
+      }
+      const uint64_t inv2 = pack2(inv, inv);
+      uint32_t o0[4], o1[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t xx = pack2(x[2 * e], x[2 * e + 1]), yy = pack2(y[2 * e], y[2 * e + 1]);
+        float u0, u1, v0, v1;
+        unpack2(mul2(inv2, fma2(ca[e], xx, mul2(sa[e], yy))), u0, u1);
+        unpack2(mul2(inv2, fma2(cb[e], yy, mul2(sb[e], xx))), v0, v1);
+        o0[e] = qc_pack(u0, u1, F16);
+        o1[e] = qc_pack(v0, v1, F16);
+      }
+      if (h < q1) {
+        *reinterpret_cast<uint4*>(dst + h * D) = make_uint4(o0[0], o0[1], o0[2], o0[3]);
+        *reinterpret_cast<uint4*>(dst + h * D + HALF) = make_uint4(o1[0], o1[1], o1[2], o1[3]);
+      }
+      now[0] = then[0]; now[1] = then[1];
+    }
+  }
+}
+
+// A thread block takes the new rows of one page, for a part of the KV heads; the last blocks of the grid take queries.
+//
+// Keys and values: a team of TEAM warps takes a KV head at a time.  A row lies in D / 16 lanes (eight elements of its first half and eight of its
+// second, so that a lane has both elements of the pairs it rotates), a team takes TEAM * 512 / D rows in a pass and keeps up to PASSES passes in
+// registers until the largest magnitude of all of them is known.  Keys are computed in fp64: their largest magnitude decides an integer, and against a
+// definition in 64 bits only 64 bits decide it alike.  The angles of the block's tokens are computed once for all heads (TABLE).  Values need no
+// arithmetic before their maximum.
+// Queries decide nothing: fp32, with angles reduced in fp64.  A warp takes a token and all of the block's query heads (where there are fewer tokens than
+// warps, a part of them), with the weights and the angles multiplied out once: x' = inv (a x + b y).
+template <int D, bool F16, int TEAM, int PASSES, bool TABLE>
+__global__ void __launch_bounds__(QA_THREADS, PASSES == 1 ? 3 : PASSES == 2 ? 2 : 1)
+qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows r, const __grid_constant__ QcFreq freq, int places, int groups, int heads_per,
+                 int kv_blocks, int q_places, int q_groups, int q_heads_per) {
+  constexpr int LPR = D / 16;                         // lanes per row
   constexpr int RPW = 32 / LPR;                       // rows of a warp in a pass
   constexpr int HALF = D / 2;
-  extern __shared__ uint8_t qa_smem[];
+  constexpr int TEAMS = QA_WARPS / TEAM;
+  extern __shared__ __align__(16) uint8_t qa_smem[];
+  __shared__ uint32_t s_size[2][QA_WARPS];
+  __shared__ uint32_t s_bnd[TEAM > 1 ? QA_WARPS : 1][2][TEAM > 1 ? HALF : 1];
+  double2* tab = reinterpret_cast<double2*>(qa_smem); // [new rows][8][LPR] cos, sin of a lane's eighth e of the pairs: what lanes read together lies together
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane % LPR, sub = lane / LPR;
-  const bool f16 = r.f16 != 0;
-
-  if ((int)blockIdx.x >= kv_blocks) {                 // ---- queries: q_rows rows of the batch
-    __shared__ int s_pos[16], s_has[16];
-    float2* tab = reinterpret_cast<float2*>(qa_smem); // [q_rows][HALF] cos, sin
-    const int base = ((int)blockIdx.x - kv_blocks) * q_rows;
-    if (tid < 16) s_pos[tid] = s_has[tid] = 0;
-    __syncthreads();
-    for (int s = tid; s < c.n_seq; s += QA_THREADS) {
-      const QcSeq q = qc_seq(c, s);
-      for (int i = max(q.r0, base); i < min(q.r0 + q.rows, base + q_rows); ++i) {
-        const int slot = q.slot0 + i - q.r0;
-        if (slot >= 0 && slot < c.limit) { s_pos[i - base] = r.positions ? r.positions[i] : slot; s_has[i - base] = 1; }
-      }
-    }
-    __syncthreads();
-    if (r.rope) {
-      for (int i = tid; i < q_rows * HALF; i += QA_THREADS) {
-        const double a = s_pos[i / HALF] * freq.over_pi[i % HALF];
-        float sn, cs;
-        sincospif((float)(a - 2.0 * rint(0.5 * a)), &sn, &cs);
-        tab[i] = make_float2(cs, sn);
-      }
-      __syncthreads();
-    }
-    float w[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = r.qw ? r.qw[lr * 4 + (e & 3) + (e >> 2) * HALF] : 1.f;
-    constexpr int PER = QA_THREADS / LPR, U = 4;      // rows (of one head) of the block in a pass; passes whose loads go out together
-    const int n = q_rows * r.Hq;
-    for (int i0 = warp * RPW + sub; i0 - sub < n; i0 += PER * U) {
-      uint2 raw[U][2];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * PER, t = i / r.Hq, h = i % r.Hq;
-        raw[u][0] = raw[u][1] = make_uint2(0, 0);
-        if (i < n && s_has[t]) {
-          const unsigned short* src = r.q + (size_t)(base + t) * r.q_stride + h * D + lr * 4;
-          raw[u][0] = *reinterpret_cast<const uint2*>(src);
-          raw[u][1] = *reinterpret_cast<const uint2*>(src + HALF);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * PER, t = min(i, n - 1) / r.Hq, h = i % r.Hq;
-        float x[8];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const float2 a = qc_elems(raw[u][hf].x, f16), b = qc_elems(raw[u][hf].y, f16);
-          x[hf * 4] = a.x; x[hf * 4 + 1] = a.y; x[hf * 4 + 2] = b.x; x[hf * 4 + 3] = b.y;
-        }
-        if (r.qw) {
-          float ss = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
-#pragma unroll
-          for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-          const float inv = 1.f / sqrtf(ss * (1.f / D) + (float)r.eps);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= inv * w[e];
-        }
-        if (r.rope) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 cs = tab[t * HALF + lr * 4 + e];
-            const float a = x[e], b = x[e + 4];
-            x[e] = a * cs.x - b * cs.y;
-            x[e + 4] = b * cs.x + a * cs.y;
-          }
-        }
-        if (i < n && s_has[t]) {
-          unsigned short* dst = r.q_out + (size_t)(base + t) * r.qo_stride + h * D + lr * 4;
-          *reinterpret_cast<uint2*>(dst) = make_uint2(qc_pack(x[0], x[1], f16), qc_pack(x[2], x[3], f16));
-          *reinterpret_cast<uint2*>(dst + HALF) = make_uint2(qc_pack(x[4], x[5], f16), qc_pack(x[6], x[7], f16));
-        }
-      }
-    }
+  if ((int)blockIdx.x >= kv_blocks) {
+    qc_append_queries<D, F16>(c, r, freq, blockIdx.x - kv_blocks, q_places, q_groups, q_heads_per, reinterpret_cast<float2*>(qa_smem));
     return;
   }
-
-  // ---- keys and values: one page's new rows, heads_per heads
-  constexpr int TEAMS = QA_WARPS / TEAM;
-  __shared__ double s_max[QA_WARPS];
-  __shared__ uint32_t s_bnd[TEAM > 1 ? QA_WARPS : 1][2][TEAM > 1 ? HALF : 1];
-  double2* tab = reinterpret_cast<double2*>(qa_smem); // [new rows][HALF] cos, sin
   const int team = warp / TEAM, tw = warp % TEAM;
   int at = blockIdx.x;
   const int grp = at % groups; at /= groups;
@@ -149,104 +198,121 @@ qc_append_kernel(const QcDev c, const QcRows r, const __grid_constant__ QcFreq f
     if (TEAM == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TEAM * 32) : "memory");
   };
-  auto angle = [&](int t, int i) {
+  auto turns = [&](int t, int i) {                    // of token t's pair i, in units of pi
     const int p = r.positions ? r.positions[row0 + t] : a + t;
-    double2 cs;
-    sincospi(p * freq.over_pi[i], &cs.y, &cs.x);
-    return cs;
+    return p * freq.over_pi[i];
   };
+  const int h0 = grp * heads_per, h1 = min(h0 + heads_per, c.Hkv);
+  auto h2 = [](uint32_t w) { return *reinterpret_cast<__half2*>(&w); };
+  auto u2 = [](__half2 w) { return *reinterpret_cast<uint32_t*>(&w); };
+  // a head's keys are asked for as soon as those of the head before have been taken over, its values as those of the one before have been written
+  uint4 kraw[PASSES][2], vraw[PASSES][2];
+  auto ask = [&](const unsigned short* from, long long stride, int h, uint4 (*raw)[2]) {
+#pragma unroll
+    for (int u = 0; u < PASSES; ++u) {
+      const int t = (u * TEAM + tw) * RPW + sub;
+      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+      if (t < nt && h < h1) {
+        const unsigned short* src = from + (size_t)(row0 + t) * stride + h * D + lr * 8;
+        raw[u][0] = *reinterpret_cast<const uint4*>(src);
+        raw[u][1] = *reinterpret_cast<const uint4*>(src + HALF);
+      }
+    }
+  };
+  ask(r.k, r.k_stride, h0 + team, kraw);
+  ask(r.v, r.v_stride, h0 + team, vraw);
   if (TABLE && r.rope) {
-    for (int i = tid; i < nt * HALF; i += QA_THREADS) tab[i] = angle(i / HALF, i % HALF);
+    for (int i = tid; i < nt * HALF; i += QA_THREADS) {
+      double2 cs;
+      sincospi(turns(i / HALF, i % HALF), &cs.y, &cs.x);
+      tab[i / HALF * HALF + i % 8 * LPR + i % HALF / 8] = cs;
+    }
     __syncthreads();
   }
-  const int h1 = min((grp + 1) * heads_per, c.Hkv);
-  for (int h = grp * heads_per + team; h < h1; h += TEAMS) {
+  for (int h = h0 + team; h < h1; h += TEAMS) {
     const size_t unit = (size_t)pid * c.Hkv + h;
     float2 old_scale = make_float2(1.f, 1.f);
     if (kept) old_scale = *reinterpret_cast<const float2*>(c.scales + unit * 2);
-    uint2 kraw[PASSES][2], vraw[PASSES][2];
+    auto key_rows = [&](int u, int t, double* y) {    // a row's part, normalised and rotated
+      float f[16];
+      qc_elems8<F16>(kraw[u][0], f);
+      qc_elems8<F16>(kraw[u][1], f + 8);
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u) {
-      const int t = (u * TEAM + tw) * RPW + sub;
-      kraw[u][0] = kraw[u][1] = vraw[u][0] = vraw[u][1] = make_uint2(0, 0);
-      if (t < nt) {
-        const unsigned short* ks = r.k + (size_t)(row0 + t) * r.k_stride + h * D + lr * 4;
-        const unsigned short* vs = r.v + (size_t)(row0 + t) * r.v_stride + h * D + lr * 4;
-        kraw[u][0] = *reinterpret_cast<const uint2*>(ks);
-        kraw[u][1] = *reinterpret_cast<const uint2*>(ks + HALF);
-        vraw[u][0] = *reinterpret_cast<const uint2*>(vs);
-        vraw[u][1] = *reinterpret_cast<const uint2*>(vs + HALF);
-      }
-    }
-    float x[PASSES][8];
-    double kmax = 0.0;
-#pragma unroll
-    for (int u = 0; u < PASSES; ++u) {
-      const int t = (u * TEAM + tw) * RPW + sub;
-      double y[8];
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const float2 e0 = qc_elems(kraw[u][hf].x, f16), e1 = qc_elems(kraw[u][hf].y, f16);
-        y[hf * 4] = e0.x; y[hf * 4 + 1] = e0.y; y[hf * 4 + 2] = e1.x; y[hf * 4 + 3] = e1.y;
-      }
+      for (int e = 0; e < 16; ++e) y[e] = f[e];
       if (r.kw) {
-        double ss = 0.0;
+        double s0 = 0.0, s1 = 0.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss += y[e] * y[e];
+        for (int e = 0; e < 16; e += 2) { s0 = fma(y[e], y[e], s0); s1 = fma(y[e + 1], y[e + 1], s1); }
+        s0 += s1;
 #pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const double inv = 1.0 / sqrt(ss * (1.0 / D) + r.eps);
+        for (int o = 1; o < LPR; o <<= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+        const double inv = qc_rsqrt(s0 * (1.0 / D) + r.eps);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= inv * (double)r.kw[lr * 4 + (e & 3) + (e >> 2) * HALF];
+        for (int e = 0; e < 16; ++e) y[e] *= inv * (double)r.kw[lr * 8 + (e & 7) + (e >> 3) * HALF];
       }
       if (r.rope && t < nt) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const double2 cs = TABLE ? tab[t * HALF + lr * 4 + e] : angle(t, lr * 4 + e);
-          const double p = y[e], m = y[e + 4];
+        for (int e = 0; e < 8; ++e) {
+          double2 cs;
+          if (TABLE) cs = tab[t * HALF + e * LPR + lr];
+          else sincospi(turns(t, lr * 8 + e), &cs.y, &cs.x);
+          const double p = y[e], m = y[e + 8];
           y[e] = p * cs.x - m * cs.y;
-          y[e + 4] = m * cs.x + p * cs.y;
+          y[e + 8] = m * cs.x + p * cs.y;
         }
       }
+    };
+    float x[PASSES][16];
+    uint32_t ksize = 0, vsize = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float f = (float)y[e];
-        if (fabs(y[e]) < INFINITY) {                  // (finite in 64 bits)
-          kmax = fmax(kmax, fabs(y[e]));
-          if (!(fabsf(f) < INFINITY)) f = copysignf(3.402823466e38f, f);
-        }
-        x[u][e] = f;
+    for (int u = 0; u < PASSES; ++u) {
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+        for (uint32_t w : {vraw[u][hf].x, vraw[u][hf].y, vraw[u][hf].z, vraw[u][hf].w}) vsize = __vmaxu2(vsize, qc_sizes(w));
+      double y[16];
+      key_rows(u, (u * TEAM + tw) * RPW + sub, y);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        ksize = max(ksize, qc_size(y[e]));
+        x[u][e] = (float)y[e];
       }
     }
-    float vmax = 0.f;
+    vsize = max(vsize & 0xffff, vsize >> 16);
+    const bool odd = __any_sync(0xffffffffu, ksize >= QC_FAR64 || vsize >= QC_INF16<F16>);      // something may not be finite: all over, more carefully
+    if (odd) {
+      ksize = vsize = 0;
 #pragma unroll
-    for (int u = 0; u < PASSES; ++u)
+      for (int u = 0; u < PASSES; ++u) {
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const float2 e0 = qc_elems(vraw[u][hf].x, f16), e1 = qc_elems(vraw[u][hf].y, f16);
-        for (float f : {e0.x, e0.y, e1.x, e1.y}) if (fabsf(f) < INFINITY) vmax = fmaxf(vmax, fabsf(f));
+        for (int hf = 0; hf < 2; ++hf)
+          for (uint32_t w : {vraw[u][hf].x, vraw[u][hf].y, vraw[u][hf].z, vraw[u][hf].w})
+            for (uint32_t one : {qc_sizes(w) & 0xffff, qc_sizes(w) >> 16}) if (one < QC_INF16<F16>) vsize = max(vsize, one);
+        double y[16];
+        key_rows(u, (u * TEAM + tw) * RPW + sub, y);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float f = (float)y[e];
+          if (fabs(y[e]) < INFINITY) {
+            ksize = max(ksize, qc_size(y[e]));
+            if (!(fabsf(f) < INFINITY)) f = copysignf(3.402823466e38f, f);      // finite in 64 bits, but not in 32: the largest that 32 hold
+          }
+          x[u][e] = f;
+        }
       }
+    }
+    vsize = __float_as_uint(F16 ? __half2float(__ushort_as_half((unsigned short)vsize)) : __uint_as_float(vsize << 16));
+    ask(r.k, r.k_stride, h + TEAMS, kraw);
     // the team's largest magnitudes
-    double vm = vmax;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      kmax = fmax(kmax, __shfl_xor_sync(0xffffffffu, kmax, o));
-      vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, o));
-    }
-    vm = vmax;
+    ksize = __reduce_max_sync(0xffffffffu, ksize);
+    vsize = __reduce_max_sync(0xffffffffu, vsize);
     if (TEAM > 1) {
-      if (lane == 0) s_max[warp] = kmax;
+      if (lane == 0) { s_size[0][warp] = ksize; s_size[1][warp] = vsize; }
       team_sync();
 #pragma unroll
-      for (int o = 0; o < TEAM; ++o) kmax = fmax(kmax, s_max[team * TEAM + o]);
-      team_sync();
-      if (lane == 0) s_max[warp] = vm;
-      team_sync();
-#pragma unroll
-      for (int o = 0; o < TEAM; ++o) vm = fmax(vm, s_max[team * TEAM + o]);
-      team_sync();
+      for (int o = 0; o < TEAM; ++o) { ksize = max(ksize, s_size[0][team * TEAM + o]); vsize = max(vsize, s_size[1][team * TEAM + o]); }
+      if (!c.bounds || kept) team_sync();             // (the words are written again, and rows may be rounded again, behind a meeting of the team)
     }
-    int ek = qc_exponent(kmax), ev = qc_exponent(vm);
+    int ek = qc_exponent64(ksize), ev = qc_exponent32(vsize);
     const int ek0 = qc_scale_exponent(old_scale.x), ev0 = qc_scale_exponent(old_scale.y);
     if (kept) { ek = max(ek, ek0); ev = max(ev, ev0); }
     uint8_t* kdst = c.codes + unit * 2 * c.page * D;
@@ -268,83 +334,103 @@ qc_append_kernel(const QcDev c, const QcRows r, const __grid_constant__ QcFreq f
     }
     // codes of the new rows; bounds from the codes, as pairs of fp16
     const uint32_t PINF2 = 0x7c007c00u, NINF2 = 0xfc00fc00u;
-    uint32_t lo[4] = {PINF2, PINF2, PINF2, PINF2}, hi[4] = {NINF2, NINF2, NINF2, NINF2};
-    const float km = pow2f(-ek), vmul = pow2f(-ev);
-    auto h2 = [](uint32_t w) { return *reinterpret_cast<__half2*>(&w); };
-    auto u2 = [](__half2 w) { return *reinterpret_cast<uint32_t*>(&w); };
+    uint32_t lo[8], hi[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { lo[e] = PINF2; hi[e] = NINF2; }
+    const float km = pow2f(-ek), vm = pow2f(-ev);
 #pragma unroll
     for (int u = 0; u < PASSES; ++u) {
       const int t = (u * TEAM + tw) * RPW + sub;
       if (t < nt) {
-        const size_t off = (size_t)(kept + t) * D + lr * 4;
+        const size_t off = (size_t)(kept + t) * D + lr * 8;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          const uint32_t w = qc_codes(x[u][hf * 4] * km, x[u][hf * 4 + 1] * km, x[u][hf * 4 + 2] * km, x[u][hf * 4 + 3] * km);
-          *reinterpret_cast<uint32_t*>(kdst + off + hf * HALF) = w;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const __half2 v = h2(e ? e4m3x2_hi_to_f16x2(w) : e4m3x2_to_f16x2(w));
-            const uint32_t num = u2(v) & __heq2_mask(v, v);        // NaN counts as 0
-            lo[hf * 2 + e] = u2(__hmin2(h2(lo[hf * 2 + e]), h2(num)));
-            hi[hf * 2 + e] = u2(__hmax2(h2(hi[hf * 2 + e]), h2(num)));
+          const float* y = x[u] + hf * 8;
+          uint2 w;
+          if (odd) {
+            w.x = qc_codes(y[0] * km, y[1] * km, y[2] * km, y[3] * km);
+            w.y = qc_codes(y[4] * km, y[5] * km, y[6] * km, y[7] * km);
+          } else {
+            w.x = qc_codes_finite(y[0] * km, y[1] * km, y[2] * km, y[3] * km);
+            w.y = qc_codes_finite(y[4] * km, y[5] * km, y[6] * km, y[7] * km);
           }
-          const float2 e0 = qc_elems(vraw[u][hf].x, f16), e1 = qc_elems(vraw[u][hf].y, f16);
-          *reinterpret_cast<uint32_t*>(vdst + off + hf * HALF) = qc_codes(e0.x * vmul, e0.y * vmul, e1.x * vmul, e1.y * vmul);
+          *reinterpret_cast<uint2*>(kdst + off + hf * HALF) = w;
+          const uint32_t num[4] = {e4m3x2_to_f16x2(w.x), e4m3x2_hi_to_f16x2(w.x), e4m3x2_to_f16x2(w.y), e4m3x2_hi_to_f16x2(w.y)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t v = odd ? num[e] & __heq2_mask(h2(num[e]), h2(num[e])) : num[e];      // NaN counts as 0
+            lo[hf * 4 + e] = u2(__hmin2(h2(lo[hf * 4 + e]), h2(v)));
+            hi[hf * 4 + e] = u2(__hmax2(h2(hi[hf * 4 + e]), h2(v)));
+          }
+          float g[8];
+          qc_elems8<F16>(vraw[u][hf], g);
+          if (odd) {
+            w.x = qc_codes(g[0] * vm, g[1] * vm, g[2] * vm, g[3] * vm);
+            w.y = qc_codes(g[4] * vm, g[5] * vm, g[6] * vm, g[7] * vm);
+          } else {
+            w.x = qc_codes_finite(g[0] * vm, g[1] * vm, g[2] * vm, g[3] * vm);
+            w.y = qc_codes_finite(g[4] * vm, g[5] * vm, g[6] * vm, g[7] * vm);
+          }
+          *reinterpret_cast<uint2*>(vdst + off + hf * HALF) = w;
         }
       }
     }
+    ask(r.v, r.v_stride, h + TEAMS, vraw);
     if (tw == 0 && lane == 0) *reinterpret_cast<float2*>(c.scales + unit * 2) = make_float2(pow2f(ek), pow2f(ev));
     if (!c.bounds) continue;
 #pragma unroll
     for (int o = LPR; o < 32; o <<= 1)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 8; ++e) {
         lo[e] = u2(__hmin2(h2(lo[e]), h2(__shfl_xor_sync(0xffffffffu, lo[e], o))));
         hi[e] = u2(__hmax2(h2(hi[e]), h2(__shfl_xor_sync(0xffffffffu, hi[e], o))));
       }
     if (TEAM > 1) {
       if (sub == 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at2 = lr * 2 + (e & 1) + (e >> 1) * (HALF / 2);
-          s_bnd[warp][0][at2] = lo[e];
-          s_bnd[warp][1][at2] = hi[e];
+        for (int e = 0; e < 8; ++e) {
+          const int pair = lr * 4 + (e & 3) + (e >> 2) * (HALF / 2);
+          s_bnd[warp][0][pair] = lo[e];
+          s_bnd[warp][1][pair] = hi[e];
         }
       }
       team_sync();
-      if (tw == 0) {
+      if (tw == 0 && sub == 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int at2 = lr * 2 + (e & 1) + (e >> 1) * (HALF / 2);
+        for (int e = 0; e < 8; ++e) {
+          const int pair = lr * 4 + (e & 3) + (e >> 2) * (HALF / 2);
+#pragma unroll
           for (int o = 1; o < TEAM; ++o) {
-            lo[e] = u2(__hmin2(h2(lo[e]), h2(s_bnd[team * TEAM + o][0][at2])));
-            hi[e] = u2(__hmax2(h2(hi[e]), h2(s_bnd[team * TEAM + o][1][at2])));
+            lo[e] = u2(__hmin2(h2(lo[e]), h2(s_bnd[team * TEAM + o][0][pair])));
+            hi[e] = u2(__hmax2(h2(hi[e]), h2(s_bnd[team * TEAM + o][1][pair])));
           }
         }
       }
       team_sync();
     }
     if (tw == 0 && sub == 0) {
-      uint8_t* b = c.bounds + unit * 2 * D + lr * 4;
+      uint8_t* b = c.bounds + unit * 2 * D + lr * 8;
 #pragma unroll
       for (int side = 0; side < 2; ++side)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t* dst = reinterpret_cast<uint32_t*>(b + side * D + hf * HALF);
-          uint32_t w0 = side ? hi[hf * 2] : lo[hf * 2], w1 = side ? hi[hf * 2 + 1] : lo[hf * 2 + 1];
-          if (kept) {                                 // bounds of the rows that were there, in the new scale
-            uint32_t o = *dst;
-            if (ek != ek0) {
-              const float m = pow2f(ek0 - ek);
-              const float2 l2 = qc_half2(e4m3x2_to_f16x2(o)), g2 = qc_half2(e4m3x2_hi_to_f16x2(o));
-              o = qc_codes(l2.x * m, l2.y * m, g2.x * m, g2.y * m);
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t* dst = reinterpret_cast<uint32_t*>(b + side * D + hf * HALF) + e;
+            uint32_t w0 = side ? hi[hf * 4 + e * 2] : lo[hf * 4 + e * 2], w1 = side ? hi[hf * 4 + e * 2 + 1] : lo[hf * 4 + e * 2 + 1];
+            if (kept) {                               // bounds of the rows that were there, in the new scale
+              uint32_t o = *dst;
+              if (ek != ek0) {
+                const float m = pow2f(ek0 - ek);
+                const float2 l2 = qc_half2(e4m3x2_to_f16x2(o)), g2 = qc_half2(e4m3x2_hi_to_f16x2(o));
+                o = qc_codes(l2.x * m, l2.y * m, g2.x * m, g2.y * m);
+              }
+              const __half2 o0 = h2(e4m3x2_to_f16x2(o)), o1 = h2(e4m3x2_hi_to_f16x2(o));
+              w0 = u2(side ? __hmax2(h2(w0), o0) : __hmin2(h2(w0), o0));
+              w1 = u2(side ? __hmax2(h2(w1), o1) : __hmin2(h2(w1), o1));
             }
-            const __half2 o0 = h2(e4m3x2_to_f16x2(o)), o1 = h2(e4m3x2_hi_to_f16x2(o));
-            w0 = u2(side ? __hmax2(h2(w0), o0) : __hmin2(h2(w0), o0));
-            w1 = u2(side ? __hmax2(h2(w1), o1) : __hmin2(h2(w1), o1));
+            *dst = f16x4_to_e4m3x4(w0, w1);
           }
-          *dst = f16x4_to_e4m3x4(w0, w1);
-        }
     }
   }
 }
@@ -537,43 +623,44 @@ qc_select_kernel(const QcDev c, int keep, int first, int recent, const unsigned 
 
 template <int D>
 struct QcAppendPlan {
-  using K = void (*)(const QcDev, const QcRows, const QcFreq, int, int, int, int, int);
+  using K = void (*)(const QcDev, const QcRows, const QcFreq, int, int, int, int, int, int, int);
   K kern;
   int teams, table_rows;
 };
 // By the new rows a page can receive: few (single tokens, short drafts) leave a warp a head to itself, so that a block's eight warps take
-// eight heads at once; 16 or 32 rows two warps; beyond that all eight warps share a head.  Above 64 rows a table of angles does not fit
+// eight heads at once; up to 16 or 32 rows four warps; beyond that all eight warps share a head.  Above 64 rows a table of angles does not fit
 // beside others on an SM; each lane then computes its own.
-template <int D>
+template <int D, bool F16>
 QcAppendPlan<D> qc_append_plan(int rows) {
-  constexpr int RPW = 256 / D;
-  if (rows <= RPW) return {qc_append_kernel<D, 1, 1, true>, 8, RPW};
-  if (rows <= 8 * RPW) return {qc_append_kernel<D, 2, 4, true>, 4, 8 * RPW};
-  if (rows <= 64) return {qc_append_kernel<D, 8, 32 / RPW / 4, true>, 1, 64};
-  if (rows <= 128) return {qc_append_kernel<D, 8, 64 / RPW / 4, false>, 1, 0};
-  return {qc_append_kernel<D, 8, 128 / RPW / 4, false>, 1, 0};
+  constexpr int RPW = 512 / D;
+  if (rows <= RPW) return {qc_append_kernel<D, F16, 1, 1, true>, 8, RPW};
+  if (rows <= 4 * RPW) return {qc_append_kernel<D, F16, 4, 1, true>, 2, 4 * RPW};
+  if (rows <= 64) return {qc_append_kernel<D, F16, 8, 8 / RPW, true>, 1, 64};
+  if (rows <= 128) return {qc_append_kernel<D, F16, 8, 16 / RPW, false>, 1, 0};
+  return {qc_append_kernel<D, F16, 8, 32 / RPW, false>, 1, 0};
 }
 
 template <int D>
 int qc_append(const QcDev& c, const QcRows& r, const QcFreq& f, cudaStream_t s) {
   const int rows = c.page < c.max_rows ? c.page : c.max_rows;
-  const QcAppendPlan<D> plan = qc_append_plan<D>(rows);
+  const QcAppendPlan<D> plan = r.f16 ? qc_append_plan<D, true>(rows) : qc_append_plan<D, false>(rows);
   const long long places = ((long long)c.max_rows + c.page - 2) / c.page + 1;      // pages that max_rows new tokens can touch
   // heads of a page together share the table of angles; apart where that leaves SMs without a block
   int heads_per = c.Hkv;
-  while (heads_per > plan.teams && places * c.n_seq * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
-  if (heads_per < plan.teams) heads_per = plan.teams;
+  while (heads_per > 1 && places * c.n_seq * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
   const int groups = (c.Hkv + heads_per - 1) / heads_per;
   const long long kv = places * c.n_seq * groups;
-  int q_rows = 1;
-  while (q_rows < 16 && c.n_rows / (q_rows * 2) >= 296) q_rows *= 2;
-  const long long qb = r.q ? ((long long)c.n_rows + q_rows - 1) / q_rows : 0;
+  const long long q_places = r.q ? ((long long)c.max_rows + QA_QROWS - 1) / QA_QROWS : 0;
+  int q_heads = r.Hq;
+  while (q_heads > 512 / D && q_places * c.n_seq * ((r.Hq + q_heads - 1) / q_heads) < 296) q_heads = (q_heads + 1) / 2;
+  const int q_groups = r.q ? (r.Hq + q_heads - 1) / q_heads : 1;
+  const long long qb = q_places * c.n_seq * q_groups;
   if (kv + qb > 0x7fffffff) return GP_ERR_INVALID;
   size_t smem = r.rope ? (size_t)plan.table_rows * (D / 2) * sizeof(double2) : 0;
-  const size_t qsmem = r.rope ? (size_t)q_rows * (D / 2) * sizeof(float2) : 0;
-  if (qsmem > smem) smem = qsmem;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(plan.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
-  plan.kern<<<(unsigned)(kv + qb), QA_THREADS, smem, s>>>(c, r, f, (int)places, groups, heads_per, (int)kv, q_rows);
+  const size_t q_smem = r.rope && r.q ? (size_t)(c.max_rows < QA_QROWS ? c.max_rows : QA_QROWS) * (D / 2) * sizeof(float2) : 0;
+  if (q_smem > smem) smem = q_smem;
+  if (smem > 32 * 1024 && cudaFuncSetAttribute(plan.kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;
+  plan.kern<<<(unsigned)(kv + qb), QA_THREADS, smem, s>>>(c, r, f, (int)places, groups, heads_per, (int)kv, (int)q_places, q_groups, q_heads);
   return cudaGetLastError() == cudaSuccess ? GP_OK : GP_ERR_CUDA;
 }
 
