@@ -436,11 +436,143 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
 }
 
 // ================================================================================================ select
-constexpr int QS_CHUNK = 128;                // pages a scoring block takes
-constexpr int QS_THREADS = 128;
-constexpr int QS_SEL_THREADS = 512;
+constexpr int QS_THREADS = 128;              // of a scoring block
+constexpr int QS_SEL_THREADS = 256;
+constexpr int QS_BITS = 11;                  // of a key that a step of the descent looks at
 constexpr int QS_CAP = 8192;                 // scores of a unit that the selection keeps in shared memory
+constexpr int QS_CLOSE = 256;                // pages close to the border that are ranked in shared memory
 constexpr double QS_UP = 0x1p860, QS_DOWN = 0x1p156;      // QS_UP * QS_DOWN = 2^1016
+constexpr float QS_ERR = 0x1p-16f * 448.f;   // error of a first score, of its scale times the sum of the weights' magnitudes (see there)
+
+// The integers that come out of the selection are those of scores in fp64; but only near the border does it take fp64 to know on which side a page lies.
+// So the tensor cores compute a first score with a bound on its error (a third of the time of fp64 throughout, which is bound by turning codes into
+// doubles: 52 us for 48 rows over 1375 pages and 8 heads), and the selection takes pages in fp64 only where those bounds leave it open.
+
+// sum of max(q, 0) and of min(q, 0) over the group, of one channel
+__device__ __forceinline__ double2 qs_weights(const unsigned short* q, int G, int D, bool f16) {      // (low's, high's)
+  double2 w = make_double2(0.0, 0.0);
+  for (int g = 0; g < G; ++g) {
+    const double x = qc_elem(q[(size_t)g * D], f16);
+    w.y += fmax(x, 0.0); w.x += fmin(x, 0.0);
+  }
+  return w;
+}
+
+// First scores of `chunk` pages for one (row, KV head): both kinds of sums are one product of the page's 2 d codes with the weights
+// [sum of min(q, 0), sum of max(q, 0)], whatever the group.  Pages are the rows of the products, codes fp16 (exact), the weights two columns: fp16, and
+// what that leaves times 2^11.  A lane reads 16 codes of a page at a time; the weights are read in the order in which four lanes then have them.
+// Error: the weights are off by 2^-22 of the largest, a product adds 16 exact terms to an fp32 sum, which it may cut off instead of rounding, so each
+// of the 2 d / 16 products is off by less than 17 * 2^-23 of what it adds up; together below 2^-17 of the sum of magnitudes, which is at most
+// 448 times the scale times the weights' sum of magnitudes: QS_ERR is twice that.  Both numbers are kept times 2^-30 (and the weights' power of two),
+// where fp32 holds them for every scale.
+template <int D>
+__global__ void __launch_bounds__(QS_THREADS)
+qc_score_kernel(const __grid_constant__ QcDev c, const unsigned short* __restrict__ q, long long q_stride, int Hq, int f16, int keep, int first, int recent,
+                float2* __restrict__ scores, int chunks, int chunk, int key_stride) {
+  constexpr int LD = 2 * D / 64;                      // 16-byte pieces of a page that a lane reads
+  constexpr int STEP = QS_THREADS / 32 * 16;          // pages of the block in a round
+  __shared__ __align__(16) __half s_w[2][2 * D];
+  __shared__ int s_seq;
+  __shared__ float s_max[QS_THREADS / 32], s_sum[QS_THREADS / 32];
+  const int part = blockIdx.x % chunks, unit = blockIdx.x / chunks, row = unit / c.Hkv, h = unit % c.Hkv, G = Hq / c.Hkv;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = lane & 3;
+  const int s = qc_seq_of_row(c, row, &s_seq);
+  gp_pdl_launch_dependents();
+  if (s < 0) return;
+  const QcSeq sq = qc_seq(c, s);
+  const int vis = min(sq.slot0 + row - sq.r0 + 1, c.limit);
+  const int m = vis > 0 ? (vis + c.page - 1) >> c.page_log : 0;
+  const int p0 = max(part * chunk, first), p1 = min((part + 1) * chunk, m - recent);
+  if (m <= keep || p0 >= p1) return;
+  const int* table = c.table + (size_t)s * c.stride;
+  const size_t page_bytes = (size_t)c.Hkv * 2 * D;
+  const uint8_t* src = c.bounds + (size_t)h * 2 * D + quad * 16;
+  int p = p0 + warp * 16 + (lane >> 2);               // this lane's pages: p and p + 8
+  auto id_of = [&](int at) {
+    const int id = at < p1 ? table[at] : -1;
+    return (unsigned)id < (unsigned)c.n_pages ? id : -1;
+  };
+  int id[2] = {id_of(p), id_of(p + 8)};
+  // weights: thread i has channel i of both kinds
+  float mx = 0.f, sum = 0.f;
+  double2 w = make_double2(0.0, 0.0);
+  if (tid < D) {
+    w = qs_weights(q + (size_t)row * q_stride + (size_t)h * G * D + tid, G, D, f16 != 0);
+    mx = fmaxf((float)-w.x, (float)w.y);
+    sum = (float)(w.y - w.x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  }
+  if (lane == 0) { s_max[warp] = mx; s_sum[warp] = sum; }
+  __syncthreads();
+  mx = 0.f; sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < QS_THREADS / 32; ++i) { mx = fmaxf(mx, s_max[i]); sum += s_sum[i]; }
+  const int up = min(14 - max((int)(__float_as_uint(mx) >> 23) - 127, -100), 114);      // 2^up brings the largest to 2^14 .. 2^15
+  const double mul = __hiloint2double((1023 + up) << 20, 0);
+  if (tid < D) {
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+      const double x = (side ? w.y : w.x) * mul;
+      const __half hi = __float2half_rn((float)x);
+      s_w[0][side * D + tid] = hi;
+      s_w[1][side * D + tid] = __float2half_rn((float)((x - (double)__half2float(hi)) * 2048.0));
+    }
+  }
+  const float err = sum * __uint_as_float((uint32_t)(127 + up) << 23) * QS_ERR;
+  uint4 x[2][LD];
+  float sc[2];
+  auto fetch = [&](const int* of) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint8_t* from = src + (size_t)max(of[k], 0) * page_bytes;
+#pragma unroll
+      for (int i = 0; i < LD; ++i) x[k][i] = *reinterpret_cast<const uint4*>(from + i * 64);
+      sc[k] = of[k] >= 0 ? c.scales[((size_t)of[k] * c.Hkv + h) * 2] : -1.f;
+    }
+  };
+  fetch(id);
+  int next[2] = {id_of(p + STEP), id_of(p + STEP + 8)};
+  __syncthreads();
+  uint32_t b[LD * 4][2];                              // column lane / 4: the weights, what they leave, nothing
+#pragma unroll
+  for (int i = 0; i < LD * 4; ++i) {
+    b[i][0] = b[i][1] = 0;
+    if (lane < 8) {
+      const uint2 v = *reinterpret_cast<const uint2*>(&s_w[lane >> 2][(i >> 2) * 64 + quad * 16 + (i & 3) * 4]);
+      b[i][0] = v.x; b[i][1] = v.y;
+    }
+  }
+  for (; p - (lane >> 2) < p1; p += STEP) {
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const uint32_t r0[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w}, r1[4] = {x[1][i].x, x[1][i].y, x[1][i].z, x[1][i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        mma_f16(acc, e4m3x2_to_f16x2(r0[e]), e4m3x2_to_f16x2(r1[e]), e4m3x2_hi_to_f16x2(r0[e]), e4m3x2_hi_to_f16x2(r1[e]), b[i * 4 + e][0], b[i * 4 + e][1]);
+    }
+    const float s0 = sc[0], s1 = sc[1];
+    const int at = p;
+    fetch(next);
+    next[0] = id_of(p + 2 * STEP); next[1] = id_of(p + 2 * STEP + 8);
+    if (quad == 0) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int pg = at + 8 * k;
+        if (pg >= p1) continue;
+        const float scale = (k ? s1 : s0) * 0x1p-30f;
+        if (scale < 0.f && c.status) atomicOr(c.status, GP_E_BOUNDS);
+        // (a page that is not there: below everything, and known to be)
+        scores[(size_t)unit * key_stride + pg] = scale < 0.f ? make_float2(-INFINITY, 0.f)
+                                                             : make_float2(fmaf(acc[2 * k + 1], 0x1p-11f, acc[2 * k]) * scale, fmaxf(err * scale, 1e-36f));
+      }
+    }
+  }
+}
 
 // a score as an integer of the same order; what is not a number is lowest
 __device__ __forceinline__ unsigned long long qc_key(double x) {
@@ -448,78 +580,111 @@ __device__ __forceinline__ unsigned long long qc_key(double x) {
   const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
   return (b >> 63) ? ~b : b | 0x8000000000000000ull;
 }
+__device__ __forceinline__ uint32_t qc_key(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return (b >> 31) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float qc_unkey(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
-// Scores of QS_CHUNK pages for one (row, KV head).  Both kinds of sums are one dot product of 2 d terms with the page's codes, whatever
-// the group: [sum of min(q, 0), sum of max(q, 0)] . [low, high].  A code's sign and its seven other bits, put where a double has its sign
-// and the low end of its exponent, are that number times 2^-1016 (codes without an exponent included: a subnormal double), so a term is
-// two integer operations and an fp64 multiply-add.  Four lanes take a page, eight pages a warp at a time.
-template <int D>
-__global__ void __launch_bounds__(QS_THREADS)
-qc_score_kernel(const QcDev c, const unsigned short* __restrict__ q, long long q_stride, int Hq, int f16, int keep, int first, int recent,
-                unsigned long long* __restrict__ keys, int chunks, int key_stride) {
-  constexpr int CH = 2 * D / 16;                      // 16-byte pieces of a page's bounds
-  __shared__ double s_w[CH * 18];                     // 16 weights a piece, two apart from the next: no bank twice
-  __shared__ int s_seq;
-  const int chunk = blockIdx.x % chunks, unit = blockIdx.x / chunks, row = unit / c.Hkv, h = unit % c.Hkv, G = Hq / c.Hkv;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int s = qc_seq_of_row(c, row, &s_seq);
-  gp_pdl_launch_dependents();
-  if (s < 0) return;
-  const QcSeq sq = qc_seq(c, s);
-  const int vis = min(sq.slot0 + row - sq.r0 + 1, c.limit);
-  const int m = vis > 0 ? (vis + c.page - 1) >> c.page_log : 0;
-  const int p0 = max(chunk * QS_CHUNK, first), p1 = min((chunk + 1) * QS_CHUNK, m - recent);
-  if (m <= keep || p0 >= p1) return;
-  for (int i = tid; i < D; i += QS_THREADS) {
-    double plus = 0.0, minus = 0.0;
-    for (int g = 0; g < G; ++g) {
-      const double x = qc_elem(q[(size_t)row * q_stride + (size_t)(h * G + g) * D + i], f16 != 0);
-      plus += fmax(x, 0.0); minus += fmin(x, 0.0);
-    }
-    s_w[(i >> 4) * 18 + (i & 15)] = minus * QS_UP;
-    s_w[((i + D) >> 4) * 18 + (i & 15)] = plus * QS_UP;
+struct QsShared {
+  int hist[1 << QS_BITS];
+  int seq, bin, left, count, close, page[QS_CLOSE];
+  unsigned long long lo[QS_SEL_THREADS / 32], hi[QS_SEL_THREADS / 32], sum[QS_SEL_THREADS / 32], key[QS_CLOSE];
+  float err[QS_SEL_THREADS / 32];
+};
+// What the threads before this one have of a sum, and what all have.
+__device__ __forceinline__ unsigned long long qs_scan(QsShared& sh, unsigned long long mine, unsigned long long* all = nullptr) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  unsigned long long upto = mine, total = 0;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
   }
   __syncthreads();
-  const int quad = lane & 3;
-  for (int p = p0 + warp * 8 + (lane >> 2); p - (lane >> 2) < p1; p += QS_THREADS / 4) {
-    const int id = p < p1 ? qc_page(c, s, p) : -1;
-    const size_t u = ((size_t)max(id, 0) * c.Hkv + h);
-    const uint4* src = reinterpret_cast<const uint4*>(c.bounds + u * 2 * D);
-    uint4 w[CH / 4];
+  if (lane == 31) sh.sum[warp] = upto;
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < CH / 4; ++i) w[i] = src[i * 4 + quad];
-    const float sc = c.scales[u * 2];
-    double acc = 0.0, acc2 = 0.0;
-#pragma unroll
-    for (int i = 0; i < CH / 4; ++i) {
-      const double* ws = s_w + (i * 4 + quad) * 18;
-      const uint32_t word[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-      for (int b = 0; b < 16; b += 2) {
-        const double2 wt = *reinterpret_cast<const double2*>(ws + b);
-        const uint32_t y0 = word[b >> 2] << (24 - 8 * (b & 3)), y1 = word[b >> 2] << (16 - 8 * (b & 3));
-        acc = fma(__hiloint2double(((int)y0 >> 7) & 0x80fe0000, 0), wt.x, acc);
-        acc2 = fma(__hiloint2double(((int)y1 >> 7) & 0x80fe0000, 0), wt.y, acc2);
-      }
-    }
-    acc += acc2;
-    acc += __shfl_xor_sync(0xffffffffu, acc, 1);
-    acc += __shfl_xor_sync(0xffffffffu, acc, 2);
-    if (quad == 0 && p < p1) keys[(size_t)unit * key_stride + p] = id < 0 ? 0ull : qc_key(acc * QS_DOWN * (double)sc);
+  for (int w = 0; w < QS_SEL_THREADS / 32; ++w) {
+    if (w < warp) upto += sh.sum[w];
+    total += sh.sum[w];
   }
+  if (all) *all = total;
+  return upto - mine;
+}
+// The want-th highest of n keys (1 <= want <= n): a radix descent from the first bit in which they differ, 11 bits at a time.  *thr: its known bits, *known:
+// which those are, returns how many of the keys equal to it there are wanted.  hist is zero before and after.
+template <typename K, typename Get>
+__device__ __forceinline__ int qs_descend(QsShared& sh, int n, int want, Get get, K* thr_out, K* known_out) {
+  constexpr int BINS = 1 << QS_BITS, PER = BINS / QS_SEL_THREADS, W = sizeof(K) * 8;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  K lo = ~(K)0, hi = 0;
+  for (int i = tid; i < n; i += QS_SEL_THREADS) {
+    const K k = get(i);
+    lo = min(lo, k); hi = max(hi, k);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+  }
+  __syncthreads();
+  if (lane == 0) { sh.lo[warp] = lo; sh.hi[warp] = hi; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < QS_SEL_THREADS / 32; ++w) { lo = min(lo, (K)sh.lo[w]); hi = max(hi, (K)sh.hi[w]); }
+  K thr = lo, known = ~(K)0;
+  int left = want;
+  const K diff = lo ^ hi;
+  if (diff) {
+    int top = 64 - __clzll((unsigned long long)diff);      // bits below this one differ
+    known = top == W ? (K)0 : (K)(~(K)0 << top);
+    thr = hi & known;
+    while (top > 0) {
+      const int bits = min(QS_BITS, top), sh2 = top - bits;
+      for (int i = tid; i < n; i += QS_SEL_THREADS) {
+        const K x = get(i);
+        if ((x & known) == thr) atomicAdd(&sh.hist[(int)(x >> sh2) & ((1 << bits) - 1)], 1);
+      }
+      __syncthreads();
+      int cnt[PER], sum = 0;                          // bins from above
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        cnt[e] = sh.hist[BINS - 1 - (tid * PER + e)];
+        sum += cnt[e];
+      }
+      int before = (int)qs_scan(sh, (unsigned long long)sum);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const int b = BINS - 1 - (tid * PER + e);
+        if (before < left && before + cnt[e] >= left) { sh.bin = b; sh.left = left - before; sh.count = cnt[e]; }
+        before += cnt[e];
+        sh.hist[b] = 0;
+      }
+      __syncthreads();
+      thr |= (K)sh.bin << sh2;
+      known |= (K)((1 << bits) - 1) << sh2;
+      left = sh.left;
+      top = sh2;
+      if (sh.count == left) break;                    // the whole bin is wanted
+    }
+  }
+  *thr_out = thr; *known_out = known;
+  return left;
 }
 
-// One block per (row, KV head): the k-th highest key by a radix descent from the first bit in which keys differ, eight bits at a time, then
-// the pages above it and the lowest of those equal to it, in ascending order.
+// One block per (row, KV head): the pages whose first score is above the border by more than the errors, and as many of those closer to it as are
+// wanted, by their scores in fp64; in ascending order (a thread takes a run of pages, one scan says where each run's go).
+template <int D>
 __global__ void __launch_bounds__(QS_SEL_THREADS)
-qc_select_kernel(const QcDev c, int keep, int first, int recent, const unsigned long long* __restrict__ keys, int key_stride,
-                 int* __restrict__ pages) {
-  extern __shared__ unsigned long long s_key[];
-  __shared__ int s_seq, s_hist[256], s_gt[QS_SEL_THREADS / 32], s_eq[QS_SEL_THREADS / 32], s_bin, s_left, s_count;
-  __shared__ unsigned long long s_lo, s_hi;
-  const int unit = blockIdx.x, row = unit / c.Hkv;
+qc_select_kernel(const __grid_constant__ QcDev c, const unsigned short* __restrict__ q, long long q_stride, int Hq, int f16, int keep, int first, int recent,
+                 float2* scores, int key_stride, int* __restrict__ pages) {
+  extern __shared__ uint32_t s_key[];
+  __shared__ QsShared sh;
+  __shared__ __align__(16) double s_w[2 * D];
+  const int unit = blockIdx.x, row = unit / c.Hkv, h = unit % c.Hkv, G = Hq / c.Hkv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int s = qc_seq_of_row(c, row, &s_seq);
+  const int s = qc_seq_of_row(c, row, &sh.seq);
   gp_pdl_launch_dependents();
   if (s < 0) { gp_pdl_wait(); return; }
   const QcSeq sq = qc_seq(c, s);
@@ -528,96 +693,134 @@ qc_select_kernel(const QcDev c, int keep, int first, int recent, const unsigned 
   int* out = pages + (size_t)unit * keep;
   if (m <= keep) {
     for (int i = tid; i < keep; i += QS_SEL_THREADS) out[i] = i < m ? i : -1;
-    gp_pdl_wait();                                  // no block ends before the kernel in front of it
+    gp_pdl_wait();                                    // no block ends before the kernel in front of it
     return;
   }
   for (int i = tid; i < first; i += QS_SEL_THREADS) out[i] = i;
   for (int i = tid; i < recent; i += QS_SEL_THREADS) out[keep - recent + i] = m - recent + i;
   const int want = keep - first - recent, n = m - first - recent;        // want < n
+  for (int i = tid; i < 1 << QS_BITS; i += QS_SEL_THREADS) sh.hist[i] = 0;
+  if (tid == 0) sh.close = 0;
   gp_pdl_wait();
   if (want == 0) return;
-  const unsigned long long* src = keys + (size_t)unit * key_stride + first;
+  float2* src = scores + (size_t)unit * key_stride + first;
   const bool near = n <= QS_CAP;
-  if (tid == 0) { s_lo = ~0ull; s_hi = 0ull; }
-  __syncthreads();
-  unsigned long long lo = ~0ull, hi = 0ull;
+  float err = 0.f;
   for (int i = tid; i < n; i += QS_SEL_THREADS) {
-    const unsigned long long k = src[i];
-    if (near) s_key[i] = k;
-    lo = min(lo, k); hi = max(hi, k);
+    const float2 x = __ldcg(src + i);
+    if (near) s_key[i] = qc_key(x.x);
+    err = fmaxf(err, x.y);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  if (lane == 0) { atomicMin(&s_lo, lo); atomicMax(&s_hi, hi); }
+  for (int o = 16; o > 0; o >>= 1) err = fmaxf(err, __shfl_xor_sync(0xffffffffu, err, o));
+  if (lane == 0) sh.err[warp] = err;
   __syncthreads();
-  const unsigned long long* k = near ? s_key : src;
-  // thr: the want-th highest key; ties: how many of its equals are wanted
-  unsigned long long thr = s_lo, known = ~0ull;     // bits of the threshold that are known
-  int left = want;
-  const unsigned long long diff = s_lo ^ s_hi;
-  if (diff) {
-    int top = 64 - __clzll(diff);                   // bits below this one differ
-    known = top == 64 ? 0ull : ~0ull << top;
-    thr = s_hi & known;
-    while (top > 0) {
-      const int bits = min(8, top), sh = top - bits;
-      for (int i = tid; i < 256; i += QS_SEL_THREADS) s_hist[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += QS_SEL_THREADS) {
-        const unsigned long long x = k[i];
-        if ((x & known) == thr) atomicAdd(&s_hist[(int)(x >> sh) & ((1 << bits) - 1)], 1);
-      }
-      __syncthreads();
-      if (warp == 0) {                              // the bin, from above, in which the count passes what is left
-        int cnt[8], sum = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { cnt[e] = s_hist[255 - (lane * 8 + e)]; sum += cnt[e]; }
-        int upto = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, upto, o);
-          if (lane >= o) upto += y;
-        }
-        int before = upto - sum;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (before < left && before + cnt[e] >= left) { s_bin = 255 - (lane * 8 + e); s_left = left - before; s_count = cnt[e]; }
-          before += cnt[e];
-        }
-      }
-      __syncthreads();
-      thr |= (unsigned long long)s_bin << sh;
-      known |= (unsigned long long)((1 << bits) - 1) << sh;
-      left = s_left;
-      top = sh;
-      if (s_count == left) break;                   // the whole bin is wanted
-    }
+  for (int w = 0; w < QS_SEL_THREADS / 32; ++w) err = fmaxf(err, sh.err[w]);
+  auto key = [&](int i) { return near ? s_key[i] : qc_key(__ldcg(src + i).x); };
+  uint32_t thr, known;
+  int left = qs_descend<uint32_t>(sh, n, want, key, &thr, &known);
+  // The want-th highest first score lies between the least and the greatest key with these bits; a page further than two errors from there is decided.
+  const float far = 2.0001f * err;
+  const uint32_t above = qc_key(qc_unkey(thr | ~known) + far), below = qc_key(qc_unkey(thr) - far);      // above: certain, below: certainly not
+  const int run = (n + QS_SEL_THREADS - 1) / QS_SEL_THREADS, i0 = min(tid * run, n), i1 = min(i0 + run, n);
+  int gt = 0, eq = 0;
+  for (int i = i0; i < i1; ++i) {
+    const uint32_t x = key(i);
+    gt += x > above; eq += x <= above && x >= below;
   }
-  // keys with known bits above thr's, and the first `left` of those equal in them, in order
-  int done = first;                                 // places filled
-  for (int base = 0; base < n; base += QS_SEL_THREADS) {
-    const int i = base + tid;
-    const unsigned long long x = i < n ? (k[i] & known) : 0ull;
-    const bool gt = i < n && x > thr, eq = i < n && x == thr;
-    const unsigned bg = __ballot_sync(0xffffffffu, gt), be = __ballot_sync(0xffffffffu, eq);
-    __syncthreads();
-    if (lane == 0) { s_gt[warp] = __popc(bg); s_eq[warp] = __popc(be); }
-    __syncthreads();
-    int g0 = 0, e0 = 0, gall = 0, eall = 0;
+  unsigned long long all, ahead = qs_scan(sh, (unsigned long long)gt << 32 | (unsigned)eq, &all);
+  const int close = (int)(unsigned)all;
+  left = want - (int)(all >> 32);                     // pages wanted of the close ones
+  if (close == left) {                                // all of them
+    int at = first + (int)(ahead >> 32) + (int)(unsigned)ahead;
+    for (int i = i0; i < i1; ++i)
+      if (key(i) >= below) out[at++] = first + i;
+    return;
+  }
+  for (int i = tid; i < D; i += QS_SEL_THREADS) {
+    const double2 w = qs_weights(q + (size_t)row * q_stride + (size_t)h * G * D + i, G, D, f16 != 0);
+    s_w[i] = w.x * QS_UP;
+    s_w[i + D] = w.y * QS_UP;
+  }
+  // a page's score in fp64, by a warp.  A code's sign and its seven other bits, put where a double has its sign and the low end of its exponent, are that
+  // number times 2^-1016 (codes without an exponent included: a subnormal double)
+  auto exact = [&](int page) {
+    const int id = c.table[(size_t)s * c.stride + page];
+    if ((unsigned)id >= (unsigned)c.n_pages) return 0ull;
+    const size_t u = (size_t)id * c.Hkv + h;
+    const uint32_t* b = reinterpret_cast<const uint32_t*>(c.bounds + u * 2 * D);
+    double acc = 0.0;
 #pragma unroll
-    for (int w = 0; w < QS_SEL_THREADS / 32; ++w) {
-      if (w < warp) { g0 += s_gt[w]; e0 += s_eq[w]; }
-      gall += s_gt[w]; eall += s_eq[w];
+    for (int i = 0; i < 2 * D / 128; ++i) {
+      const uint32_t word = b[i * 32 + lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        acc = fma(__hiloint2double(((int)(word << (24 - 8 * e)) >> 7) & 0x80fe0000, 0), s_w[(i * 32 + lane) * 4 + e], acc);
     }
-    const unsigned below = (1u << lane) - 1;
-    const int er = e0 + __popc(be & below);         // equals before this one, in this stretch
-    const int at = done + g0 + __popc(bg & below) + min(er, left);
-    if (gt || (eq && er < left)) out[at] = first + i;
-    done += gall + min(eall, left);
-    left -= min(eall, left);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+    return qc_key(acc * QS_DOWN * (double)c.scales[u * 2]);
+  };
+  if (close <= QS_CLOSE) {
+    int at = (int)(unsigned)ahead;                    // the close pages, in their order
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t x = key(i);
+      if (x <= above && x >= below) sh.page[at++] = i;
+    }
+    __syncthreads();
+    for (int i = warp; i < close; i += QS_SEL_THREADS / 32) {
+      const unsigned long long k = exact(first + sh.page[i]);
+      if (lane == 0) sh.key[i] = k;
+    }
+    __syncthreads();
+    bool taken = false;
+    if (tid < close) {                                // one that fewer than `left` are ahead of
+      const unsigned long long mine = sh.key[tid];
+      int better = 0;
+      for (int i = 0; i < close; ++i) better += sh.key[i] > mine || (sh.key[i] == mine && i < tid);
+      taken = better < left;
+    }
+    __syncthreads();
+    if (tid < close) sh.key[tid] = taken;
+    __syncthreads();
+    // places: certain pages and taken ones before this thread's run
+    int mine = 0, nth = (int)(unsigned)ahead;
+    for (int i = nth; i < nth + eq; ++i) mine += (int)sh.key[i];
+    at = first + (int)(ahead >> 32) + (int)qs_scan(sh, (unsigned long long)mine);
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t x = key(i);
+      if (x > above) out[at++] = first + i;
+      else if (x >= below && sh.key[nth++]) out[at++] = first + i;
+    }
+    return;
+  }
+  // many close pages (equal ones, or one of a scale far above the others'): 64-bit keys in the scores' place, all ones for the certain pages
+  unsigned long long* keys = reinterpret_cast<unsigned long long*>(src);
+  __syncthreads();
+  for (int i = warp; i < n; i += QS_SEL_THREADS / 32) {
+    const uint32_t x = key(i);
+    unsigned long long k = x > above ? ~0ull : 0ull;
+    if (x <= above && x >= below) k = max(exact(first + i), 1ull);
+    __syncwarp();
+    if (lane == 0) __stcg(keys + i, k);
+  }
+  __threadfence_block();
+  __syncthreads();
+  auto key64 = [&](int i) { return __ldcg(keys + i); };
+  unsigned long long thr64, known64;
+  left = qs_descend<unsigned long long>(sh, n, want, key64, &thr64, &known64);
+  gt = eq = 0;
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long x = key64(i) & known64;
+    gt += x > thr64; eq += x == thr64;
+  }
+  ahead = qs_scan(sh, (unsigned long long)gt << 32 | (unsigned)eq);
+  int eqs = (int)(unsigned)ahead, at = first + (int)(ahead >> 32) + min(eqs, left);
+  for (int i = i0; i < i1; ++i) {
+    const unsigned long long x = key64(i) & known64;
+    if (x > thr64) out[at++] = first + i;
+    else if (x == thr64 && eqs++ < left) out[at++] = first + i;
   }
 }
 
@@ -724,20 +927,25 @@ extern "C" int gp_qcache_select(const gp_qcache* cache, const gp_qbatch* batch, 
   if (qc_empty(c)) return GP_OK;
   const long long units = (long long)c.n_rows * c.Hkv;
   const int stride = (int)(((long long)c.limit + c.page - 1) / c.page);
-  const long long chunks = stride > keep ? (stride + QS_CHUNK - 1) / QS_CHUNK : 0;
+  // a block prepares its weights for as many pages as leave the GPU four rounds of blocks (eight an SM), 128 at least
+  long long chunk = ((long long)stride * units / (4 * 148 * 8) + 127) / 128 * 128;
+  if (chunk < 128) chunk = 128;
+  const long long chunks = stride > keep ? (stride + chunk - 1) / chunk : 0;
   if (units * (chunks ? chunks : 1) > 0x7fffffff) return GP_ERR_INVALID;
   QcDevice dev(cache->device);
   if (!dev.ok) return GP_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  unsigned long long* keys = static_cast<unsigned long long*>(work);
+  float2* scores = static_cast<float2*>(work);
+  const unsigned short* qp = static_cast<const unsigned short*>(q);
+  const int f16 = type == GP_TYPE_F16;
   if (chunks) {
     auto score = cache->head_dim == 128 ? qc_score_kernel<128> : qc_score_kernel<64>;
-    score<<<(unsigned)(units * chunks), QS_THREADS, 0, s>>>(c, static_cast<const unsigned short*>(q), q_stride, n_q_heads, type == GP_TYPE_F16, keep, first,
-                                                           recent, keys, (int)chunks, stride);
+    score<<<(unsigned)(units * chunks), QS_THREADS, 0, s>>>(c, qp, q_stride, n_q_heads, f16, keep, first, recent, scores, (int)chunks, (int)chunk, stride);
     if (cudaGetLastError() != cudaSuccess) return GP_ERR_CUDA;
   }
-  const size_t smem = (size_t)(stride < QS_CAP ? stride : QS_CAP) * 8;
-  if (smem > 40 * 1024 && cudaFuncSetAttribute(qc_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, QS_CAP * 8) != cudaSuccess) return GP_ERR_CUDA;
-  return gp_launch(qc_select_kernel, (int)units, QS_SEL_THREADS, smem, s, chunks > 0, c, (int)keep, (int)first, (int)recent,
-                   static_cast<const unsigned long long*>(keys), stride, static_cast<int*>(pages)) == cudaSuccess ? GP_OK : GP_ERR_CUDA;
+  auto select = cache->head_dim == 128 ? qc_select_kernel<128> : qc_select_kernel<64>;
+  const size_t smem = (size_t)(stride < QS_CAP ? stride : QS_CAP) * 4;
+  if (smem > 16 * 1024 && cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, QS_CAP * 4) != cudaSuccess) return GP_ERR_CUDA;
+  return gp_launch(select, (int)units, QS_SEL_THREADS, smem, s, chunks > 0, c, qp, (long long)q_stride, (int)n_q_heads, f16, (int)keep, (int)first, (int)recent, scores,
+                   stride, static_cast<int*>(pages)) == cudaSuccess ? GP_OK : GP_ERR_CUDA;
 }
