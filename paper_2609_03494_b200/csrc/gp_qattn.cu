@@ -6,15 +6,16 @@
 
 namespace {
 
-constexpr int QT_STAGES = 2;                   // stages of a warp's ring
+__host__ __device__ constexpr int qt_stages(int d) { return d == 64 ? 4 : 2; }      // stages of a warp's ring: 16 KB
 constexpr int QT_TILES = 2;                    // tiles of 16 tokens in a stage
 constexpr int QT_GRANULE = QT_WARPS * QT_TILES * 16;
 constexpr int QT_MIN_SHARE = 2;                // granules a thread block takes at least
 constexpr int QT_UNIT = 2;                     // what a unit costs beside its granules, in granules (its queries, the way to its first page, its end)
 constexpr float QT_LIFT = 8.f;                 // weights are carried times 2^8 ...
+constexpr float QT_NONE = -3.3e38f;            // a maximum of nothing
 constexpr float QT_SLACK = 7.f;                // ... while no logit is further above the maximum they refer to than this (base 2)
 
-constexpr int qt_resident(int nt, int d) { return nt * d <= 128 ? 3 : 2; }      // blocks of an SM that the registers allow
+constexpr int qt_resident(int nt, int d) { return nt * d <= 192 ? 3 : 2; }      // blocks of an SM that the registers allow
 
 __device__ __forceinline__ uint32_t qt_transpose8x8(uint32_t x) {
   uint32_t y;
@@ -39,6 +40,7 @@ __device__ __forceinline__ int qt_granules(const QcDev& c, const QtArgs& a, cons
 template <bool LIST>
 __device__ __forceinline__ long long qt_head_granules(const QcDev& c, const QtArgs& a, const QcSeq& q) {     // of one KV head of a sequence
   if (LIST) return (long long)q.rows * (qt_granules<LIST>(c, a, q, 0) + QT_UNIT);
+  if (q.rows * a.G > a.few) return 0;                  // the other kernel's
   long long g = 0;
   for (int t = 0; t * a.rows_tile < q.rows; ++t) g += qt_granules<LIST>(c, a, q, t) + QT_UNIT;
   return g;
@@ -64,13 +66,13 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
   constexpr int CH = D / 16;                            // 16-byte pieces of a token's codes
   constexpr int ST = D + 2;
   constexpr int ROWS = 16 * D;                          // bytes of a tile's keys, or values
-  constexpr int STAGE = QT_TILES * 2 * ROWS;
+  constexpr int STAGE = QT_TILES * 2 * ROWS, STAGES = qt_stages(D);
   extern __shared__ uint8_t smem_raw[];
   __shared__ long long s_upto[QT_THREADS], s_warp[QT_WARPS];
-  __shared__ __align__(8) uint64_t s_bar[QT_WARPS][QT_STAGES];
+  __shared__ __align__(8) uint64_t s_bar[QT_WARPS][STAGES];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // (the swizzle goes by the address)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (tid < QT_WARPS * QT_STAGES) mbar_init(&s_bar[0][0] + tid, 1);
+  if (tid < QT_WARPS * STAGES) mbar_init(&s_bar[0][0] + tid, 1);
   fence_mbar_init();
   if (LIST) gp_pdl_wait();                              // the list may come from the kernel before
   gp_pdl_launch_dependents();
@@ -110,7 +112,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
   QcSeq sq = qc_seq(c, seq);
   long long per_head = qt_head_granules<LIST>(c, a, sq);
   const float norm = 1.4426950408889634f * rsqrtf((float)D);
-  const uint32_t ring = smem_u32(smem) + warp * QT_STAGES * STAGE;
+  const uint32_t ring = smem_u32(smem) + warp * STAGES * STAGE;
   uint32_t phases = 0;                                  // parity of each stage's barrier
   bool gave_up = false;
 
@@ -195,14 +197,14 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
       const int tok = __shfl_sync(0xffffffffu, now ? cur.tok : nxt.tok, j & 31);
       const int left = __shfl_sync(0xffffffffu, now ? cur.left : nxt.left, j & 31);
       const bool mine = lane < 2 * QT_TILES && left > 0;
-      const uint32_t bar = smem_u32(&s_bar[warp][i % QT_STAGES]);
+      const uint32_t bar = smem_u32(&s_bar[warp][i % STAGES]);
       const int n = __popc(__ballot_sync(0xffffffffu, mine));
-      if (lane == 0) mbar_expect_tx(&s_bar[warp][i % QT_STAGES], n * ROWS);
+      if (lane == 0) mbar_expect_tx(&s_bar[warp][i % STAGES], n * ROWS);
       __syncwarp();
-      if (mine) qt_tma_rows(ring + (i % QT_STAGES) * STAGE + lane * ROWS, &map, (u.h * 2 + (lane & 1)) * c.page + (tok & (c.page - 1)), id, bar);
+      if (mine) qt_tma_rows(ring + (i % STAGES) * STAGE + lane * ROWS, &map, (u.h * 2 + (lane & 1)) * c.page + (tok & (c.page - 1)), id, bar);
     };
 #pragma unroll
-    for (int i = 0; i < QT_STAGES - 1; ++i) fetch(i, 0);
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i, 0);
 
     // queries: column n = lane / 4 of each tile, codes 4 (lane % 4) .. + 3 of every 16
     uint32_t qb[NT][CH][2];
@@ -247,7 +249,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int j = 0; j < CH; ++j) o[n][j][0] = o[n][j][1] = o[n][j][2] = o[n][j][3] = 0.f;
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = QT_NONE;
       l[n][0] = l[n][1] = 0.f;
     }
 
@@ -261,70 +263,81 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         nxt = look((batch + 1) * 32 + lane);
         look_scales(nxt);
       }
-      fetch(i + QT_STAGES - 1, batch);
+      fetch(i + STAGES - 1, batch);
       {
-        const int st = i % QT_STAGES;
+        const int st = i % STAGES;
         for (unsigned spin = 0; !mbar_try_wait(&s_bar[warp][st], (phases >> st) & 1); ++spin)
           if (spin > GP_SPIN_LIMIT) { gave_up = true; break; }
         phases ^= 1u << st;
       }
-      const uint32_t stage = ring + (i % QT_STAGES) * STAGE;
-      int left[QT_TILES];
-      float vs[QT_TILES];
-      float s[QT_TILES][NT][4];
-      bool over = false;
+      const uint32_t stage = ring + (i % STAGES) * STAGE;
+      int left[QT_TILES], tok[QT_TILES];
+      float kf[QT_TILES], vs[QT_TILES];                 // scales of keys and values
+      int most = 0, end = 0;
 #pragma unroll
       for (int k = 0; k < QT_TILES; ++k) {
         const int j = (i * QT_TILES + k) & 31;
         left[k] = __shfl_sync(0xffffffffu, cur.left, j);
+        kf[k] = __shfl_sync(0xffffffffu, cur.ks, j);
         vs[k] = __shfl_sync(0xffffffffu, cur.vs, j);
-        const int tok = __shfl_sync(0xffffffffu, cur.tok, j);
-        const float ks = __shfl_sync(0xffffffffu, cur.ks, j);
-        if (left[k] <= 0) continue;
-        const uint32_t kt = stage + k * 2 * ROWS + lt * D;
+        tok[k] = left[k] > 0 ? __shfl_sync(0xffffffffu, cur.tok, j) : 0x40000000;      // (a tile that is not there is seen by nobody)
+        most = max(most, left[k]); end = max(end, tok[k]);
+      }
+      if (most <= 0) { __syncwarp(); continue; }
+      float s[QT_TILES][NT][4];
+      auto factor = [&](int k, int n, int e) { return fmaxf(kf[k] * qs[n][e], 1.2e-38f); };      // (above 0: a masked logit stays what it is)
+      // (d = 64: no branch on what a tile holds lies between the tiles of a stage, so that one's instructions fill the other's waits, 73 -> 70 us for five
+      // rows of 48 sequences; d = 128 has no registers for both, 122 -> 126 us for three long sequences)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[k][n][0] = s[k][n][1] = s[k][n][2] = s[k][n][3] = 0.f;
+      for (int k = 0; k < QT_TILES; ++k) {
+        if (D == 128 && left[k] <= 0) continue;
 #pragma unroll
         for (int p = 0; p < CH / 2; ++p) {
           uint32_t r0, r1, r2, r3;                      // pieces 2p, 2p + 1 of tokens 0..7 and 8..15
-          ldsm_x4(kt + (((2 * p + (mi >> 1)) ^ lsw) << 4), r0, r1, r2, r3);
+          ldsm_x4(stage + k * 2 * ROWS + lt * D + (((2 * p + (mi >> 1)) ^ lsw) << 4), r0, r1, r2, r3);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const uint32_t xx = half ? r2 : r0, yy = half ? r3 : r1;
             const uint32_t a0 = e4m3x2_to_f16x2(xx), a2 = e4m3x2_hi_to_f16x2(xx), a1 = e4m3x2_to_f16x2(yy), a3 = e4m3x2_hi_to_f16x2(yy);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_f16(s[k][n], a0, a1, a2, a3, qb[n][2 * p + half][0], qb[n][2 * p + half][1]);
+            for (int n = 0; n < NT; ++n) {
+              if (p == 0 && half == 0) mma_f16_first(s[k][n], a0, a1, a2, a3, qb[n][0][0], qb[n][0][1]);
+              else mma_f16(s[k][n], a0, a1, a2, a3, qb[n][2 * p + half][0], qb[n][2 * p + half][1]);
+            }
           }
         }
+      }
+      if (end + 16 > vis0) {                            // some column does not see all of the stage
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const float k0 = ks * qs[n][0], k1 = ks * qs[n][1];
-          s[k][n][0] *= k0; s[k][n][1] *= k1; s[k][n][2] *= k0; s[k][n][3] *= k1;
-        }
-        if (tok + 16 > vis0) {                          // some column does not see all of the tile
+        for (int k = 0; k < QT_TILES; ++k) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (tok + (lane >> 2) + (e >> 1) * 8 >= qt_visible(c, u, a.G, n * 8 + (lane & 3) * 2 + (e & 1))) s[k][n][e] = -INFINITY;
-          if (left[k] < 16) {                           // rows behind the sequence: whatever an earlier owner left there, NaN too
-            for (int r = left[k] * (D / 16) + lane; r < D; r += 32)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (k * 2 + 1) * ROWS + r * 16), "r"(0) : "memory");
-            fence_proxy_async();                        // the next copy into the stage comes behind these stores
-            __syncwarp();
-          }
+              if (tok[k] + (lane >> 2) + (e >> 1) * 8 >= qt_visible(c, u, a.G, n * 8 + (lane & 3) * 2 + (e & 1))) s[k][n][e] = -INFINITY;
+          // rows behind the sequence, and tiles that are not there: whatever an earlier owner or tile left, NaN too
+          for (int r = max(left[k], 0) * (D / 16) + lane; r < D; r += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (k * 2 + 1) * ROWS + r * 16), "r"(0) : "memory");
         }
+        fence_proxy_async();                            // the next copy into the stage comes behind these stores
+        __syncwarp();
+      }
+      bool over = false;
+#pragma unroll
+      for (int k = 0; k < QT_TILES; ++k)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          over |= fmaxf(s[k][n][0], s[k][n][2]) > m[n][0] + (QT_LIFT + QT_SLACK) || fmaxf(s[k][n][1], s[k][n][3]) > m[n][1] + (QT_LIFT + QT_SLACK);
-      }
+          over |= fmaf(fmaxf(s[k][n][0], s[k][n][2]), factor(k, n, 0), -m[n][0]) > QT_LIFT + QT_SLACK ||
+                  fmaf(fmaxf(s[k][n][1], s[k][n][3]), factor(k, n, 1), -m[n][1]) > QT_LIFT + QT_SLACK;
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-          for (int k = 0; k < QT_TILES; ++k)
-            if (left[k] > 0) { mx[0] = fmaxf(mx[0], fmaxf(s[k][n][0], s[k][n][2])); mx[1] = fmaxf(mx[1], fmaxf(s[k][n][1], s[k][n][3])); }
+          for (int k = 0; k < QT_TILES; ++k) {
+            mx[0] = fmaxf(mx[0], fmaxf(s[k][n][0], s[k][n][2]) * factor(k, n, 0));
+            mx[1] = fmaxf(mx[1], fmaxf(s[k][n][1], s[k][n][3]) * factor(k, n, 1));
+          }
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) {
             mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], off));
@@ -344,15 +357,14 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
       }
 #pragma unroll
       for (int k = 0; k < QT_TILES; ++k) {
-        if (left[k] <= 0) continue;
-        const uint32_t vt = stage + (k * 2 + 1) * ROWS + lt * D;
+        if (D == 128 && left[k] <= 0) continue;
         uint32_t pb[NT][TERMS][2];                      // B fragments of P^T: tokens 0..7 and 8..15
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const float b0 = m[n][0] == -INFINITY ? 0.f : m[n][0], b1 = m[n][1] == -INFINITY ? 0.f : m[n][1];      // nothing seen yet: weights of 0
+          const float f0 = factor(k, n, 0), f1 = factor(k, n, 1);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const float p0 = qt_exp2(s[k][n][2 * half] - b0), p1 = qt_exp2(s[k][n][2 * half + 1] - b1);
+            const float p0 = qt_exp2(fmaf(s[k][n][2 * half], f0, -m[n][0])), p1 = qt_exp2(fmaf(s[k][n][2 * half + 1], f1, -m[n][1]));
             l[n][0] += p0; l[n][1] += p1;
             const __half2 h = __floats2half2_rn(p0, p1);
             pb[n][0][half] = qt_transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
@@ -366,16 +378,16 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
 #pragma unroll
         for (int p = 0; p < CH / 2; ++p) {
           uint32_t r0, r1, r2, r3;                      // pieces 2p, 2p + 1 of tokens 0..7 and 8..15, transposed in pairs of channels
-          ldsm_x4_t(vt + (((2 * p + (mi >> 1)) ^ lsw) << 4), r0, r1, r2, r3);
+          ldsm_x4_t(stage + (k * 2 + 1) * ROWS + lt * D + (((2 * p + (mi >> 1)) ^ lsw) << 4), r0, r1, r2, r3);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             const uint32_t xx = __byte_perm(half ? r2 : r0, 0, 0x3120), yy = __byte_perm(half ? r3 : r1, 0, 0x3120);
             const uint32_t a0 = e4m3x2_to_f16x2(xx), a1 = e4m3x2_hi_to_f16x2(xx), a2 = e4m3x2_to_f16x2(yy), a3 = e4m3x2_hi_to_f16x2(yy);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              if (TERMS == 2) mma_f16(d, a0, a1, a2, a3, pb[n][TERMS - 1][0], pb[n][TERMS - 1][1]);
-              mma_f16(d, a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
+              float d[4];
+              mma_f16_first(d, a0, a1, a2, a3, pb[n][TERMS - 1][0], pb[n][TERMS - 1][1]);
+              if (TERMS == 2) mma_f16(d, a0, a1, a2, a3, pb[n][0][0], pb[n][0][1]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) o[n][2 * p + half][e] = fmaf(d[e], vs[k], o[n][2 * p + half][e]);
             }
@@ -442,17 +454,19 @@ bool qt_map(const gp_qcache* c, CUtensorMap* map) {
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Whether the kernel for many rows takes the call.
-bool qt_many_rows(const QcDev& c, int G, bool list) { return !list && (long long)c.max_rows * G > 64; }
-
 // How a call is cut up, by sizes alone.
 struct QtPlan { int nt, blocks; };
 QtPlan qt_plan(const QcDev& c, int G, int d, int n_list, bool list) {
   QtPlan p;
-  const long long cols = list ? G : (long long)c.max_rows * G;
-  p.nt = cols <= 8 ? 1 : cols <= 16 ? 2 : cols <= 24 || d == 128 ? 3 : 4;      // (four tiles of 128 elements do not fit the registers)
+  const bool all = (long long)c.max_rows * G <= qt_few(d);                     // sequences of more rows are the other kernel's
+  const int rows = list ? 1 : all ? c.max_rows : qt_few(d) / G;
+  const long long cols = (long long)rows * G;
+  // Tiles of columns by what a sequence may have; beside sequences of many rows most have one row (255 of them beside one of 2048 rows: 272 us with single
+  // tiles, 380 with as many as 48 columns want).  (Four tiles of 128 elements do not fit the registers.)
+  p.nt = cols <= 8 || !all ? 1 : cols <= 16 ? 2 : cols <= 24 || d == 128 ? 3 : 4;
+  if (list) p.nt = 1;
   const int rows_tile = list ? 1 : p.nt * 8 / G;
-  const long long units = (long long)c.n_seq * ((c.max_rows + rows_tile - 1) / rows_tile) * c.Hkv;
+  const long long units = (long long)c.n_seq * ((list ? c.max_rows : rows) + rows_tile - 1) / rows_tile * c.Hkv;
   const long long len = list ? (long long)n_list << c.page_log : c.limit;
   const long long most = units * ((len + QT_GRANULE - 1) / QT_GRANULE + 1 + QT_UNIT);          // granules, more than there can be
   const long long wave = 148 * qt_resident(p.nt, d);
@@ -466,7 +480,7 @@ size_t qt_bytes(const QtPlan& p, int d) { return qt_joins_bytes(p) + (size_t)p.b
 template <int D, int NT, int TERMS, bool LIST>
 int qt_launch(const QcDev& c, const QtArgs& a, const CUtensorMap& map, const QtPlan& p, cudaStream_t s) {
   auto kern = qt_split_kernel<D, NT, TERMS, LIST>;
-  size_t smem = QT_WARPS * QT_STAGES * QT_TILES * 32 * D;
+  size_t smem = QT_WARPS * qt_stages(D) * QT_TILES * 32 * D;
   const size_t merge = (size_t)QT_WARPS * NT * 8 * (D + 2) * sizeof(float);
   if (merge > smem) smem = merge;
   smem += 1024;
@@ -486,15 +500,25 @@ int qt_dispatch(const QcDev& c, const QtArgs& a, const CUtensorMap& map, const Q
   }
 }
 
+// Which of the two kernels a call has work for: that for many rows where a sequence may have them; that for few unless all have as many.
+struct QtBoth { bool few, many; QtPlan few_plan; QpPlan many_plan; size_t few_bytes, bytes; };
+QtBoth qt_both(const QcDev& c, int G, int d, int n_list) {
+  QtBoth b = {};
+  const bool list = n_list > 0;
+  b.many = !list && (long long)c.max_rows * G > qt_few(d);
+  b.few = !b.many || (c.n_seq > 1 && c.n_rows < (long long)c.n_seq * c.max_rows);
+  if (b.few) { b.few_plan = qt_plan(c, G, d, n_list, list); b.few_bytes = (qt_bytes(b.few_plan, d) + 15) / 16 * 16; }
+  b.bytes = b.few_bytes;
+  if (b.many) { b.many_plan = qp_plan(c, G); b.bytes += qp_bytes(b.many_plan, d); }
+  return b;
+}
+
 }  // namespace
 
 extern "C" size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch, int32_t n_q_heads, int32_t n_list) {
   QcDev c;
   if (qc_check(cache, batch, &c) != GP_OK || n_q_heads < 1 || n_q_heads % c.Hkv || n_q_heads / c.Hkv > 8 || n_list < 0) return 0;
-  if (qc_empty(c)) return 0;
-  const int G = n_q_heads / c.Hkv;
-  if (qt_many_rows(c, G, n_list > 0)) return qp_bytes(qp_plan(c, G), cache->head_dim);
-  return qt_bytes(qt_plan(c, G, cache->head_dim, n_list, n_list > 0), cache->head_dim);
+  return qc_empty(c) ? 0 : qt_both(c, n_q_heads / c.Hkv, cache->head_dim, n_list).bytes;
 }
 
 extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batch, const void* q, int64_t q_stride, int32_t n_q_heads, int32_t type,
@@ -512,24 +536,23 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
   a.Hq = n_q_heads; a.G = n_q_heads / c.Hkv; a.f16 = type == GP_TYPE_F16;
   a.pages = pages; a.n_list = n_list;
   a.out = out; a.out_type = out_type;
-  const bool many = qt_many_rows(c, a.G, pages != nullptr);
-  if (many) {
-    const QpPlan p = qp_plan(c, a.G);
-    const size_t need = qp_bytes(p, cache->head_dim);
-    if (need && (!work || qc_misaligned(work, 16) || work_bytes < need)) return GP_ERR_INVALID;
-    QcDevice dev(cache->device);
-    return dev.ok ? qp_launch(c, a, p, cache->head_dim, work, static_cast<cudaStream_t>(stream)) : GP_ERR_CUDA;
-  }
-  const QtPlan p = qt_plan(c, a.G, cache->head_dim, n_list, pages != nullptr);
-  if (!work || qc_misaligned(work, 16) || work_bytes < qt_bytes(p, cache->head_dim)) return GP_ERR_INVALID;
-  a.joins = static_cast<int4*>(work);
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + qt_joins_bytes(p));
-  a.rows_tile = pages ? 1 : p.nt * 8 / a.G;
+  const int d = cache->head_dim;
+  a.few = qt_few(d);
+  const QtBoth b = qt_both(c, a.G, d, n_list);
+  if (!work || qc_misaligned(work, 16) || work_bytes < b.bytes) return GP_ERR_INVALID;
   QcDevice dev(cache->device);
   if (!dev.ok) return GP_ERR_CUDA;
-  CUtensorMap map;
-  if (!qt_map(cache, &map)) return GP_ERR_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (cache->head_dim == 128) return out_type == GP_TYPE_F32 ? qt_dispatch<128, 2>(c, a, map, p, s) : qt_dispatch<128, 1>(c, a, map, p, s);
-  return out_type == GP_TYPE_F32 ? qt_dispatch<64, 2>(c, a, map, p, s) : qt_dispatch<64, 1>(c, a, map, p, s);
+  if (b.few) {
+    const QtPlan& p = b.few_plan;
+    a.joins = static_cast<int4*>(work);
+    a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + qt_joins_bytes(p));
+    a.rows_tile = pages ? 1 : p.nt * 8 / a.G;
+    CUtensorMap map;
+    if (!qt_map(cache, &map)) return GP_ERR_CUDA;
+    const int got = d == 128 ? (out_type == GP_TYPE_F32 ? qt_dispatch<128, 2>(c, a, map, p, s) : qt_dispatch<128, 1>(c, a, map, p, s))
+                             : (out_type == GP_TYPE_F32 ? qt_dispatch<64, 2>(c, a, map, p, s) : qt_dispatch<64, 1>(c, a, map, p, s));
+    if (got != GP_OK) return got;
+  }
+  return b.many ? qp_launch(c, a, b.many_plan, d, static_cast<uint8_t*>(work) + b.few_bytes, s) : GP_OK;
 }

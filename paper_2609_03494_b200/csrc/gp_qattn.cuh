@@ -5,6 +5,11 @@
 constexpr int QT_WARPS = 4;
 constexpr int QT_THREADS = QT_WARPS * 32;
 
+// A sequence goes to the kernel for few rows (gp_qattn.cu) up to this many columns (row, query head of the group), beyond it to the one for many
+// (gp_qprompt.cu), whose tiles have 256.  16 sequences of 3000 tokens, 8 KV heads, us: d = 64 with 48 / 64 / 96 columns 57 / 60 / 84 in the former, 63 / 64 /
+// 65 in the latter; d = 128 with 32 / 48 / 64 columns 75 / 80 / 109 and 90 / 91 / 91.
+constexpr int qt_few(int d) { return d == 64 ? 64 : 48; }
+
 struct QtArgs {
   const unsigned short* q;
   long long q_stride;
@@ -13,6 +18,7 @@ struct QtArgs {
   void* out; int out_type;
   int4* joins;                                 // [blocks][2] what qt_merge_kernel has to do
   float* part;                                 // [blocks][2][columns][D + 2]
+  int few;                                     // qt_few
   int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
 };
 

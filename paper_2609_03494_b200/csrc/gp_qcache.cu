@@ -66,13 +66,51 @@ __device__ __forceinline__ uint32_t qc_codes_finite(float a, float b, float c, f
   return r;
 }
 
+// Which sequence job `at` is of, where each has as many as `count` says, and its number there: false if there is none.  Every thread of the block adds up a
+// run of sequences.
+template <typename Count>
+__device__ __forceinline__ bool qc_find(const QcDev& c, int at, Count count, int* seq, int* nth) {
+  __shared__ int s_upto[QA_THREADS], s_warp[QA_WARPS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, run = (c.n_seq + QA_THREADS - 1) / QA_THREADS;
+  int upto = 0;
+  for (int s = tid * run; s < min((tid + 1) * run, c.n_seq); ++s) upto += count(qc_seq(c, s));
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) s_warp[warp] = upto;
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) upto += s_warp[w];
+  s_upto[tid] = upto;
+  __syncthreads();
+  if (at >= s_upto[QA_THREADS - 1]) return false;
+  int lo = 0, hi = QA_THREADS - 1;                    // the run: first with s_upto > at
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (s_upto[mid] > at) hi = mid;
+    else lo = mid + 1;
+  }
+  int s = lo * run, before = lo ? s_upto[lo - 1] : 0;
+  for (int n; at >= before + (n = count(qc_seq(c, s))); ++s) before += n;
+  *seq = s; *nth = at - before;
+  return true;
+}
+// pages that a sequence's rows touch; stretches of QA_QROWS rows that it has
+__device__ __forceinline__ int qc_pages(const QcDev& c, const QcSeq& q) {
+  const int first = max(q.slot0, 0), end = min(q.slot0 + q.rows, c.limit);
+  return first < end ? ((end - 1) >> c.page_log) - (first >> c.page_log) + 1 : 0;
+}
+__device__ __forceinline__ int qc_stretches(const QcSeq& q) { return (q.rows + QA_QROWS - 1) / QA_QROWS; }
+
 // Queries of up to 16 rows of a sequence, for a part of the heads.
 template <int D, bool F16>
 __device__ __forceinline__ void qc_append_queries(const QcDev& c, const QcRows& r, const QcFreq& freq, int at, int places, int groups, int heads_per, float2* tab) {
   constexpr int LPR = D / 16, RPW = 32 / LPR, HALF = D / 2;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lr = lane % LPR, sub = lane / LPR;
   const int q0 = at % groups * heads_per, q1 = min(q0 + heads_per, r.Hq); at /= groups;
-  const int place = at % places, s = at / places;
+  int place = at % max(places, 1), s = at / max(places, 1);
+  if (places == 0 && !qc_find(c, at, [](const QcSeq& q) { return qc_stretches(q); }, &s, &place)) return;
   const QcSeq q = qc_seq(c, s);
   const int i0 = max(place * QA_QROWS, -q.slot0), i1 = min(min((place + 1) * QA_QROWS, q.rows), c.limit - q.slot0);      // rows that lie in a slot
   const int nt = i1 - i0;
@@ -184,7 +222,8 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
   const int team = warp / TEAM, tw = warp % TEAM;
   int at = blockIdx.x;
   const int grp = at % groups; at /= groups;
-  const int place = at % places, s = at / places;
+  int place = at % max(places, 1), s = at / max(places, 1);
+  if (places == 0 && !qc_find(c, at, [&](const QcSeq& q) { return qc_pages(c, q); }, &s, &place)) return;
   const QcSeq q = qc_seq(c, s);
   const int first = max(q.slot0, 0), end = min(q.slot0 + q.rows, c.limit);        // slots the batch fills
   const int lp = (first >> c.page_log) + place;
@@ -722,7 +761,8 @@ qc_select_kernel(const __grid_constant__ QcDev c, const unsigned short* __restri
   int left = qs_descend<uint32_t>(sh, n, want, key, &thr, &known);
   // The want-th highest first score lies between the least and the greatest key with these bits; a page further than two errors from there is decided.
   const float far = 2.0001f * err;
-  const uint32_t above = qc_key(qc_unkey(thr | ~known) + far), below = qc_key(qc_unkey(thr) - far);      // above: certain, below: certainly not
+  // (keys of numbers, the infinite ones included, lie between these two)
+  const uint32_t above = qc_key(qc_unkey(min(thr | ~known, 0xff800000u)) + far), below = qc_key(qc_unkey(max(thr, 0x007fffffu)) - far);      // above: certain, below: certainly not
   const int run = (n + QS_SEL_THREADS - 1) / QS_SEL_THREADS, i0 = min(tid * run, n), i1 = min(i0 + run, n);
   int gt = 0, eq = 0;
   for (int i = i0; i < i1; ++i) {
@@ -847,17 +887,23 @@ template <int D>
 int qc_append(const QcDev& c, const QcRows& r, const QcFreq& f, cudaStream_t s) {
   const int rows = c.page < c.max_rows ? c.page : c.max_rows;
   const QcAppendPlan<D> plan = r.f16 ? qc_append_plan<D, true>(rows) : qc_append_plan<D, false>(rows);
-  const long long places = ((long long)c.max_rows + c.page - 2) / c.page + 1;      // pages that max_rows new tokens can touch
+  // Jobs: pages that max_rows new tokens can touch, for every sequence; where that is far more than all the rows together can (one long chunk among single
+  // tokens), as many as they can, and a block looks for its own (256 sequences, one of 2048 rows: 36 us; 110 with a block for every page and sequence)
+  long long places = ((long long)c.max_rows + c.page - 2) / c.page + 1, q_places = ((long long)c.max_rows + QA_QROWS - 1) / QA_QROWS;
+  long long jobs = places * c.n_seq, q_jobs = q_places * c.n_seq;
+  const long long most = (long long)c.n_rows / c.page + 2 * (long long)c.n_seq, q_most = (long long)c.n_rows / QA_QROWS + c.n_seq;
+  if (jobs > 4 * most) { jobs = most; places = 0; }
+  if (q_jobs > 4 * q_most) { q_jobs = q_most; q_places = 0; }
+  if (!r.q) q_jobs = 0;
   // heads of a page together share the table of angles; apart where that leaves SMs without a block
   int heads_per = c.Hkv;
-  while (heads_per > 1 && places * c.n_seq * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
+  while (heads_per > 1 && jobs * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
   const int groups = (c.Hkv + heads_per - 1) / heads_per;
-  const long long kv = places * c.n_seq * groups;
-  const long long q_places = r.q ? ((long long)c.max_rows + QA_QROWS - 1) / QA_QROWS : 0;
+  const long long kv = jobs * groups;
   int q_heads = r.Hq;
-  while (q_heads > 512 / D && q_places * c.n_seq * ((r.Hq + q_heads - 1) / q_heads) < 296) q_heads = (q_heads + 1) / 2;
+  while (q_heads > 512 / D && q_jobs * ((r.Hq + q_heads - 1) / q_heads) < 296) q_heads = (q_heads + 1) / 2;
   const int q_groups = r.q ? (r.Hq + q_heads - 1) / q_heads : 1;
-  const long long qb = q_places * c.n_seq * q_groups;
+  const long long qb = q_jobs * q_groups;
   if (kv + qb > 0x7fffffff) return GP_ERR_INVALID;
   size_t smem = r.rope ? (size_t)plan.table_rows * (D / 2) * sizeof(double2) : 0;
   const size_t q_smem = r.rope && r.q ? (size_t)(c.max_rows < QA_QROWS ? c.max_rows : QA_QROWS) * (D / 2) * sizeof(float2) : 0;

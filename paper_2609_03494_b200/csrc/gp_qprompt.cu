@@ -97,7 +97,9 @@ __device__ __forceinline__ void qp_wait(QpShared& sh, uint64_t* bar, uint32_t pa
 __device__ __forceinline__ long long qp_line(const QcSeq& q, int R, long long T) {
   return T * (max(q.slot0, 0) + QP_UNIT) + R * (T * (T + 1) / 2);
 }
-__device__ __forceinline__ long long qp_head_line(const QcSeq& q, int R) { return qp_line(q, R, (q.rows + R - 1) / R); }
+__device__ __forceinline__ long long qp_head_line(const QcSeq& q, int R, const QtArgs& a) {
+  return q.rows * a.G > a.few ? qp_line(q, R, (q.rows + R - 1) / R) : 0;        // (few rows: the other kernel's)
+}
 
 struct QpPiece {                               // a stretch of a unit (one without steps has no number: nobody waits for another in it)
   QtUnit u;                                    // of all of the tile
@@ -107,11 +109,11 @@ struct QpPiece {                               // a stretch of a unit (one witho
 // Walks along a block's stretch of the line; every thread does, and keeps no more than its place between two pieces.
 struct QpWalk {
   long long x;
-  __device__ __forceinline__ bool start(const QcDev& c, int R, QpShared& sh) {
+  __device__ __forceinline__ bool start(const QcDev& c, const QtArgs& a, int R, QpShared& sh) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int run = (c.n_seq + QP_THREADS - 1) / QP_THREADS;
     long long up = 0;
-    for (int s = tid * run; s < min((tid + 1) * run, c.n_seq); ++s) up += c.Hkv * qp_head_line(qc_seq(c, s), R);
+    for (int s = tid * run; s < min((tid + 1) * run, c.n_seq); ++s) up += c.Hkv * qp_head_line(qc_seq(c, s), R, a);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const long long y = __shfl_up_sync(0xffffffffu, up, o);
@@ -145,11 +147,11 @@ struct QpWalk {
       int seq = lo * run;
       long long xs = lo ? sh.upto[lo - 1] : 0;          // where sequence `seq` begins
       QcSeq sq = qc_seq(c, seq);
-      long long per_head = qp_head_line(sq, R);
+      long long per_head = qp_head_line(sq, R, a);
       while (x >= xs + per_head * c.Hkv) {
         xs += per_head * c.Hkv;
         sq = qc_seq(c, ++seq);
-        per_head = qp_head_line(sq, R);
+        per_head = qp_head_line(sq, R, a);
       }
       QtUnit& u = p.u;
       u.seq = seq;
@@ -232,7 +234,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
   }
   qp_fence_before();
   QpWalk walk;
-  const bool any = walk.start(c, R, sh);                // (meets twice)
+  const bool any = walk.start(c, a, R, sh);                // (meets twice)
   qp_fence_after();
   gp_pdl_launch_dependents();
   const uint32_t tmem = sh.tmem;

@@ -395,6 +395,20 @@ def test_a_serving_run_prompt_tokens_drafts_and_sparse_steps():
     rig.check()
 
 
+@pytest.mark.parametrize("d,page,G,out", [(128, 16, 4, BF16), (64, 32, 8, F32), (128, 64, 3, F16)])
+def test_long_chunks_among_single_tokens_and_sequences_without_rows(d, page, G, out):
+    n = 70
+    rig = Rig(n, 6 + 400 // page, 2, d, page, seed=44 + d)
+    first = [1 + (7 * i) % 60 for i in range(n)]
+    rig.append(first)
+    rows = [1] * n
+    rows[3], rows[17], rows[18], rows[40], rows[69] = 333, 0, 170, 20, 9
+    q, ref = rig.append(rows, theta=1e4, norm=True, q_heads=2 * G)
+    rig.check()
+    q64 = f64(q)
+    check_attention(rig, rows, q, q64, rig.gpu.attention(rig.batch(rows), q, out_dtype=getattr(T(), out)), out)
+
+
 def test_a_captured_step_is_replayed_with_other_lengths_on_another_stream():
     torch = T()
     rig = Rig(3, 30, 2, 64, 16, seed=42)
