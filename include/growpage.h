@@ -482,9 +482,10 @@ typedef struct gp_qcache {
   void*    codes;            /* device e4m3 [n_pages][n_kv_heads][2: keys, values][page_size][d], 16-byte aligned      */
   float*   scales;           /* device fp32 [n_pages][n_kv_heads][2], 8-byte aligned                                   */
   void*    bounds;           /* device e4m3 [n_pages][n_kv_heads][2: low, high][d], 16-byte aligned; NULL: none kept   */
-  int32_t* status;           /* device word that the kernels set bit 4 in when a page id they met is none of the
-                                cache's (the page is then skipped: nothing is written, its tokens count as absent);
-                                NULL: not told                                                                         */
+  int32_t* status;           /* device word that the kernels set bits in (gp_pool_status's): 4 when a page id they met
+                                is none of the cache's (the page is then skipped: nothing is written, its tokens count
+                                as absent), 1 when a bounded wait inside gp_qcache_attention gave up (its results are
+                                then not meaningful); NULL: not told                                                   */
 } gp_qcache;
 
 /* A packed batch: rows row_start[s] .. row_start[s + 1] - 1 of the batch's tensors belong to sequence s and are its

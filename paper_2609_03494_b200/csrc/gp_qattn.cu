@@ -554,5 +554,6 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
                              : (out_type == GP_TYPE_F32 ? qt_dispatch<64, 2>(c, a, map, p, s) : qt_dispatch<64, 1>(c, a, map, p, s));
     if (got != GP_OK) return got;
   }
+  a.few = b.few ? qt_few(d) : 0;                        // (alone, it takes sequences of few rows too)
   return b.many ? qp_launch(c, a, b.many_plan, d, static_cast<uint8_t*>(work) + b.few_bytes, s) : GP_OK;
 }

@@ -200,7 +200,7 @@ struct QpWalk {
 // Scales of pages cost nothing per element: 16 columns of S lie in one page, so the keys' scale joins the factor of the logits and the exponent of
 // the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
 // sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
-// keeping it in range; out = 2^E O / L.
+// keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
 // What bounds it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with d = 128 the same.
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
@@ -440,7 +440,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           qp_ld32(t_x, x0);
           qp_ld32(t_x + 32, x1);
           const float4 kq = *reinterpret_cast<const float4*>(sh.ks[slot]), eq = *reinterpret_cast<const float4*>(sh.ev[slot]);
-          const float ks[4] = {kq.x, kq.y, kq.z, kq.w}, ev[4] = {eq.x, eq.y, eq.z, eq.w};
+          const float ks[4] = {kq.x, kq.y, kq.z, kq.w};
+          float ev[4] = {eq.x, eq.y, eq.z, eq.w};
           const int t0 = u.t0 + j * QP_N;
           float top = -1000.f, f[4];
           bool gone = false;
@@ -450,6 +451,15 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             if (ks[g] < 0.f) gone = true;
             else top = fmaxf(top, ev[g]);
           }
+          // E, and the exponents as far as they matter beside it: values 2^100 below E's (a page of zeros has the smallest exponent there is) may count as
+          // 2^-100 times E's, their weights count alike
+          float dE = 0.f;
+          if (top > -1000.f) {
+            if (j == 0) E = top;
+            else if (top > E + 40.f) { dE = top - E; E = top; }
+          }
+#pragma unroll
+          for (int g = 0; g < 4; ++g) ev[g] = fmaxf(ev[g], E - 100.f);
           const bool masked = __any_sync(0xffffffffu, t0 + QP_N > see) || gone;      // some row does not see all of the step
           qp_wait_ld();
           if (masked) {
@@ -468,12 +478,6 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             m0 = qp_max3(m0, x[10], x[11]); m1 = qp_max3(m1, x[12], x[13]);
             m0 = qp_max3(m0, x[14], x[15]);
             mx = fmaxf(mx, fmaf(fmaxf(m0, m1), f[g], ev[g]));
-          }
-          // maximum and E
-          float dE = 0.f;
-          if (top > -1000.f) {
-            if (j == 0) E = top;
-            else if (top > E + 40.f) { dE = top - E; E = top; }
           }
           const bool over = mx > M + (QP_LIFT + QP_SLACK);
           if (__any_sync(0xffffffffu, over || dE != 0.f)) {
@@ -523,7 +527,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             }
             float s0, s1;
             qp_unpack2(acc, s0, s1);
-            L = fmaf(s0 + s1, qt_exp2(fminf(E - ev[g], 100.f)), L);
+            L = fmaf(s0 + s1, qt_exp2(E - ev[g]), L);
             qp_st8(t_x + g * 8, hi);
             if (TERMS == 2) qp_st8(t_x + 32 + g * 8, lo);
           }

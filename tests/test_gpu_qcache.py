@@ -249,6 +249,59 @@ def test_pages_whose_values_differ_by_many_powers_of_two():
     check_attention(rig, [1], q, q64, rig.gpu.attention(rig.batch([1]), q, out_dtype=T().float32), F32)
 
 
+@pytest.mark.parametrize("d,G,out", [(128, 4, BF16), (64, 8, F32)])
+@pytest.mark.parametrize("rows", [1, 5, 40, 150])
+def test_values_of_zero_and_of_all_sizes_before_many_rows(d, G, out, rows):
+    """Pages of zeros have the smallest scale there is, others are 2^60 apart: the weights of all of them count alike."""
+    rig = Rig(1, 30, 2, d, 16, seed=60 + rows)
+    z = dev(np.zeros((48, 2, d), np.float32)).to(T().bfloat16)
+    for scale in (0, 1.0, 0, 1e-18, 1e6, 0, 30.0):
+        v = (z, f64(z)) if scale == 0 else rig.draw(48, 2, d, scale=scale)
+        rig.append([48], kv=(rig.draw(48, 2, d), v))
+    rig.append([64])
+    q, q64 = rig.draw(rows, 2 * G, d)
+    check_attention(rig, [rows], q, q64, rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)), out)
+    zero = Rig(1, 30, 2, d, 16, seed=61)                 # nothing but zeros, then a page that is not
+    zero.append([200], kv=(zero.draw(200, 2, d), (dev(np.zeros((200, 2, d), np.float32)).to(T().bfloat16), np.zeros((200, 2, d)))))
+    zero.append([40], scale=2.0)
+    check_attention(zero, [rows], q, q64, zero.gpu.attention(zero.batch([rows]), q, out_dtype=getattr(T(), out)), out)
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+def test_a_padded_batch_whose_sequences_have_fewer_rows_than_there_is_room_for(d, G):
+    torch = T()
+    rig = Rig(3, 20, 2, d, 16, seed=62)
+    rig.append([250, 30, 111])
+    q, q64 = rig.draw(300, 2 * G, d)
+    for rows in ([1, 1, 1], [100, 1, 3], [0, 2, 100], [1, 0, 0]):
+        out = torch.full((300, 2 * G, d), 5.0, dtype=torch.bfloat16, device="cuda")
+        n = sum(rows)
+        b = rig.batch(rows, max_rows=100, extra=300 - n)
+        rig.gpu.attention(b, q, out=out)
+        check_attention(rig, rows, q[:n], q64[:n], out[:n], BF16)
+        assert (out[n:] == 5).all()
+    one = Rig(1, 20, 2, d, 16, seed=63)
+    one.append([250])
+    out = torch.full((100, 2 * G, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    one.gpu.attention(one.batch([2], max_rows=100, extra=98), q[:100], out=out)
+    check_attention(one, [2], q[:2], q64[:2], out[:2], BF16)
+    assert (out[2:] == 5).all()
+
+
+def test_many_rows_that_see_nothing():
+    torch = T()
+    for d, G in ((64, 2), (128, 8)):
+        rig = Rig(2, 20, 2, d, 16, seed=64)
+        rig.append([40, 300])
+        rows, lens = [100, 120], np.array([30, 300], np.int32)      # sequence 0 claims fewer tokens than rows
+        q, q64 = rig.draw(220, 2 * G, d)
+        out = f64(rig.gpu.attention(rig.batch(rows, lens=lens), q, out_dtype=torch.float32))
+        assert (out[:70] == 0).all()
+        rig.len = lens
+        check_attention(rig, [30, 0], q[70:100], q64[70:100], torch.from_numpy(out[70:100]), F32)
+        check_attention(rig, [0, 120], q[100:], q64[100:], torch.from_numpy(out[100:]), F32)
+
+
 def test_rows_that_see_nothing_and_lengths_beyond_the_bounds():
     torch = T()
     rig = Rig(3, 4, 2, 64, 16, seed=23)
