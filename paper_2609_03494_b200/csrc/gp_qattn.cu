@@ -151,8 +151,8 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     }
     x = xu + g1;
     const int* list = LIST ? a.pages + ((size_t)u.row0 * c.Hkv + u.h) * a.n_list : nullptr;
-    const int vis = max(qt_visible(c, u, a.G, u.cols - 1), 0);           // of the last column: the most
-    const int vis0 = qt_visible(c, u, a.G, 0);                           // of the first: the least
+    const int vis = max(qt_visible(c, a, u, u.cols - 1), 0);           // of the last column: the most
+    const int vis0 = qt_visible(c, a, u, 0);                           // of the first: the least
     u.t0 = g0 * QT_GRANULE;
     u.t1 = min(LIST ? a.n_list << c.page_log : vis, g1 * QT_GRANULE);
 
@@ -214,11 +214,13 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
       const int col = n * 8 + (lane >> 2);
       float mx = 0.f;
       uint2 raw[CH];
+      const int r = qt_row(a, col);
+      const unsigned short* from = a.q + (size_t)(u.row0 + r) * a.q_stride + (size_t)(u.h * a.G + col - r * a.G) * D + (lane & 3) * 4;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
         raw[j] = make_uint2(0, 0);
         if (col < u.cols)
-          raw[j] = *reinterpret_cast<const uint2*>(a.q + (size_t)(u.row0 + col / a.G) * a.q_stride + (size_t)(u.h * a.G + col % a.G) * D + j * 16 + (lane & 3) * 4);
+          raw[j] = *reinterpret_cast<const uint2*>(from + j * 16);
       }
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
@@ -314,7 +316,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (tok[k] + (lane >> 2) + (e >> 1) * 8 >= qt_visible(c, u, a.G, n * 8 + (lane & 3) * 2 + (e & 1))) s[k][n][e] = -INFINITY;
+              if (tok[k] + (lane >> 2) + (e >> 1) * 8 >= qt_visible(c, a, u, n * 8 + (lane & 3) * 2 + (e & 1))) s[k][n][e] = -INFINITY;
           // rows behind the sequence, and tiles that are not there: whatever an earlier owner or tile left, NaN too
           for (int r = max(left[k], 0) * (D / 16) + lane; r < D; r += 32)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (k * 2 + 1) * ROWS + r * 16), "r"(0) : "memory");
@@ -533,7 +535,7 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
   QtArgs a;
   a.q = static_cast<const unsigned short*>(q);
   a.q_stride = q_stride;
-  a.Hq = n_q_heads; a.G = n_q_heads / c.Hkv; a.f16 = type == GP_TYPE_F16;
+  a.Hq = n_q_heads; a.G = n_q_heads / c.Hkv; a.by_g = qt_by_g(a.G); a.f16 = type == GP_TYPE_F16;
   a.pages = pages; a.n_list = n_list;
   a.out = out; a.out_type = out_type;
   const int d = cache->head_dim;

@@ -19,6 +19,7 @@ struct QtArgs {
   int4* joins;                                 // [blocks][2] what qt_merge_kernel has to do
   float* part;                                 // [blocks][2][columns][D + 2]
   int few;                                     // qt_few
+  unsigned by_g;                               // qt_row
   int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
 };
 
@@ -38,9 +39,17 @@ struct QtUnit {
   int t0, t1;                                  // tokens of the stretch (with a list: places of the list times the page size)
   int total;                                   // granules of the unit, on the line behind QT_UNIT more
 };
+// the row of column `col` (of 256 at most) in its tile: col / G by a multiplication, exact for col * (G - 1) < 2^16
+__device__ __forceinline__ int qt_row(const QtArgs& a, int col) { return (int)((unsigned)col * a.by_g >> 16); }
+__host__ __device__ inline unsigned qt_by_g(int G) { return (65536u + G - 1) / G; }
 // tokens that column `col` of a unit sees
-__device__ __forceinline__ int qt_visible(const QcDev& c, const QtUnit& u, int G, int col) {
-  return min(u.slot0 + col / G + 1, c.limit);
+__device__ __forceinline__ int qt_visible(const QcDev& c, const QtArgs& a, const QtUnit& u, int col) {
+  return min(u.slot0 + qt_row(a, col) + 1, c.limit);
+}
+// where column `col`'s query, or result, lies: its number among the call's (row, query head)
+__device__ __forceinline__ size_t qt_query(const QtArgs& a, const QtUnit& u, int col) {
+  const int r = qt_row(a, col);
+  return (size_t)(u.row0 + r) * a.Hq + u.h * a.G + (col - r * a.G);
 }
 // Four warps of a block (all of it, in the kernel that has no more) meet.
 __device__ __forceinline__ void qt_sync(int bar) { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); }
@@ -63,8 +72,7 @@ __device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const
       l += wt * p[D + 1];
     }
     if (!part) {
-      const size_t rh = (size_t)(u.row0 + col / a.G) * a.Hq + u.h * a.G + col % a.G;
-      qt_store(a.out, a.out_type, rh * D + e, l != 0.f ? o / l : 0.f);      // (a NaN sum is not 0)
+      qt_store(a.out, a.out_type, qt_query(a, u, col) * D + e, l != 0.f ? o / l : 0.f);      // (a NaN sum is not 0)
     } else {
       float* dst = part + (size_t)col * ST;
       dst[e] = o;
@@ -81,7 +89,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
   const int warp = (threadIdx.x >> 5) % QT_WARPS, lane = threadIdx.x & 31;
   const float scale = 1.4426950408889634f * rsqrtf((float)D);
   for (int col = 0; col < u.cols; ++col) {
-    const int row = u.row0 + col / a.G, head = u.h * a.G + col % a.G, vis = qt_visible(c, u, a.G, col);
+    const int r = qt_row(a, col), row = u.row0 + r, head = u.h * a.G + col - r * a.G, vis = qt_visible(c, a, u, col);
     float q[PER], o[PER], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int e = 0; e < PER; ++e) { q[e] = qc_elem(a.q[(size_t)row * a.q_stride + (size_t)head * D + lane + 32 * e], a.f16); o[e] = 0.f; }
@@ -112,7 +120,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
     one.cols = 1; one.row0 = row;
     if (!part) {                                        // qt_write's column 0 is this head
       QtArgs b = a;
-      b.G = 1; b.Hq = 1;
+      b.G = 1; b.Hq = 1; b.by_g = qt_by_g(1);
       one.row0 = row * a.Hq + head; one.h = 0;
       qt_write<D>(b, one, smem, 1, nullptr);
     } else {
@@ -166,7 +174,8 @@ qt_merge_kernel(const __grid_constant__ QtArgs a) {
       }
     }
   }
-  const size_t rh = ((size_t)(u.x + col / a.G) * a.Hq + u.y * a.G + col % a.G) * D;
+  const int row = qt_row(a, col);
+  const size_t rh = ((size_t)(u.x + row) * a.Hq + u.y * a.G + (col - row * a.G)) * D;
   const float inv = l != 0.f ? 1.f / l : 0.f;          // (a NaN sum is not 0)
 #pragma unroll
   for (int e = 0; e < PER; ++e) {

@@ -133,7 +133,8 @@ struct QpWalk {
     __syncthreads();
     return x < all;
   }
-  __device__ __forceinline__ bool next(const QcDev& c, const QtArgs& a, int R, const QpShared& sh, QpPiece& p, int4* join) {      // join[0], [1]: what is to be joined at its end
+  // (one copy for all warps: code that runs once a unit is fetched anew each time)  join[0], [1]: what is to be joined at its end
+  __device__ __noinline__ bool next(const QcDev& c, const QtArgs& a, int R, const QpShared& sh, QpPiece& p, int4* join) {
     const int run = (c.n_seq + QP_THREADS - 1) / QP_THREADS;
     const long long x1 = sh.x1, x0 = blockIdx.x * sh.share;
     for (;;) {
@@ -155,11 +156,14 @@ struct QpWalk {
       }
       QtUnit& u = p.u;
       u.seq = seq;
-      u.h = (int)((x - xs) / per_head);
+      // quotients and roots from fp32, put right by whole numbers
+      u.h = (int)__fdividef((float)(x - xs), (float)per_head);
+      while (u.h > 0 && u.h * per_head > x - xs) --u.h;
+      while ((u.h + 1) * per_head <= x - xs) ++u.h;
       const long long xh = xs + u.h * per_head;
-      // the tile: the root of R T^2 / 2 + (s + QP_UNIT + R / 2) T = x - xh, put right by whole numbers
-      const double b = max(sq.slot0, 0) + QP_UNIT + 0.5 * R;
-      long long T = (long long)((sqrt(b * b + 2.0 * R * (double)(x - xh)) - b) / R);
+      // the tile: the root of R T^2 / 2 + (s + QP_UNIT + R / 2) T = x - xh
+      const float b = (float)(max(sq.slot0, 0) + QP_UNIT) + 0.5f * R;
+      long long T = (long long)__fdividef(sqrtf(b * b + 2.f * R * (float)(x - xh)) - b, (float)R);
       while (T > 0 && qp_line(sq, R, T) > x - xh) --T;
       while (qp_line(sq, R, T + 1) <= x - xh) ++T;
       const long long xu = xh + qp_line(sq, R, T), xe = xh + qp_line(sq, R, T + 1);
@@ -179,7 +183,9 @@ struct QpWalk {
       u.t1 = min(vis, g1 * QP_N);
       p.n_steps = (max(u.t1 - u.t0, 0) + QP_N - 1) / QP_N;
       if (g0 > 0 && g1 == u.total) {                    // the unit began before this block and ends here
-        const int from = (int)(xu / sh.share);
+        int from = (int)__fdividef((float)xu, (float)sh.share);
+        while (from > 0 && from * sh.share > xu) --from;
+        while ((from + 1) * sh.share <= xu) ++from;
         join[0] = make_int4(u.cols, from * 2 + (xu == from * sh.share ? 0 : 1), from + 1, blockIdx.x);
         join[1] = make_int4(u.row0, u.h, 0, 0);
       }
@@ -303,7 +309,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       const QtUnit& u = p.u;
-      const int vis0 = qt_visible(c, u, a.G, 0);        // of the first row: the least
+      const int vis0 = qt_visible(c, a, u, 0);        // of the first row: the least
       const uint8_t* src = c.codes + (size_t)(u.h * 2 + kv) * c.page * D + ch * 16;
       const int* table = c.table + (size_t)u.seq * c.stride;
       // lanes 0 .. 3: page of a group of 16 tokens of a step, as the table has it (looked at a turn later: nothing waits for it here)
@@ -332,12 +338,9 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         if (!kv && ids >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((size_t)ids * c.Hkv + u.h) * 2);
       };
       const int j0 = (turn + QP_TURN - n % QP_TURN) % QP_TURN;      // its first step of the piece
-      int next = 0;
-      if (j0 < p.n_steps) {
-        load(j0, page_of(j0));
-        next = page_of(j0 + QP_TURN);
-      }
-      for (int j = j0; j < p.n_steps; j += QP_TURN) {
+      int next = page_of(j0);
+      for (int j = j0 - QP_TURN; j < p.n_steps; j += QP_TURN) {      // what the turn before asked for, then what the next will want
+        if (j >= 0) {
         const int s = n + j;
         const int at = s & (QP_RING - 1);
         if (s >= QP_RING) qp_wait(sh, empty + at, ((s - QP_RING) / QP_RING) & 1);
@@ -366,6 +369,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
+        }
         if (j + QP_TURN < p.n_steps) {
           load(j + QP_TURN, next);
           next = page_of(j + 2 * QP_TURN);
@@ -384,46 +388,45 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       u.rows = max(min(RT, u.rows - half * RT), 0);
       u.cols = u.rows * a.G;
       const bool used = u.cols > 0, real = t128 < u.cols;
-      const int see = real ? qt_visible(c, u, a.G, t128) : 0x7fffffff;
+      const int see = real ? qt_visible(c, a, u, t128) : 0x7fffffff;
       float qs = 0.f;                                   // what S is multiplied with
       if (used && p.n_steps > 0) {                      // the warp's 32 columns, D / 8 lanes a column
         constexpr int LPC = D / 8, CPR = 32 / LPC, ROUNDS = 32 / CPR;
         const int piece8 = lane % LPC;
-        // (code that runs once a unit is kept short: its instructions come from far away every time)
+        int col = (warp & 3) * 32 + lane / LPC;
+        auto place = [&](int cc) { return q_smem + half * QOPERAND + (piece8 >> 3) * QP_QBLOCK + cc * 128 + (((piece8 & 7) ^ (cc & 7)) << 4); };
+        // as they are, to where they will lie; then each brought to its scale there.  (Short loops: see QpWalk::next)
 #pragma unroll 1
-        for (int i0 = 0; i0 < ROUNDS; i0 += 4) {
-          uint4 w[4];
-          int col0 = (warp & 3) * 32 + i0 * CPR + lane / LPC;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int col = col0 + i * CPR;
-            w[i] = make_uint4(0, 0, 0, 0);
-            if (col < u.cols) w[i] = *reinterpret_cast<const uint4*>(a.q + (size_t)(u.row0 + col / a.G) * a.q_stride + (size_t)(u.h * a.G + col % a.G) * D + piece8 * 8);
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int col = col0 + i * CPR;
-            float mx = 0.f;
-            for (uint32_t e : {w[i].x, w[i].y, w[i].z, w[i].w}) { const float2 x = qc_elems(e, a.f16); mx = fmaxf(mx, fmaxf(fabsf(x.x), fabsf(x.y))); }
-#pragma unroll
-            for (int o = 1; o < LPC; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const int ex = max((int)(__float_as_uint(mx) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
-            const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
-            const float down = 1.4426950408889634f * rsqrtf((float)D) * __uint_as_float((uint32_t)(127 - up) << 23);
-            if (piece8 == 0) sh.qs[half][col & 127] = down;
-            for (uint32_t* e : {&w[i].x, &w[i].y, &w[i].z, &w[i].w}) {
-              const float2 x = qc_elems(*e, a.f16);
-              const __half2 h = __floats2half2_rn(x.x * mul, x.y * mul);
-              *e = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_smem + half * QOPERAND + (piece8 >> 3) * QP_QBLOCK + col * 128 + (((piece8 & 7) ^ (col & 7)) << 4)),
-                         "r"(w[i].x), "r"(w[i].y), "r"(w[i].z), "r"(w[i].w)
-                         : "memory");
-          }
+        for (int i = 0; i < ROUNDS; ++i, col += CPR) {
+          const int r = qt_row(a, min(col, u.cols - 1)), cc = min(col, u.cols - 1);
+          const unsigned short* from = a.q + (size_t)(u.row0 + r) * a.q_stride + (size_t)(u.h * a.G + cc - r * a.G) * D + piece8 * 8;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place(col)), "l"(from), "r"(col < u.cols ? 16 : 0) : "memory");
         }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncwarp();
+        col -= ROUNDS * CPR;
+#pragma unroll 1
+        for (int i = 0; i < ROUNDS; ++i, col += CPR) {
+          uint4 w;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place(col)));
+          float mx = 0.f;
+          for (uint32_t e : {w.x, w.y, w.z, w.w}) { const float2 x = qc_elems(e, a.f16); mx = fmaxf(mx, fmaxf(fabsf(x.x), fabsf(x.y))); }
+#pragma unroll
+          for (int o = 1; o < LPC; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const int ex = max((int)(__float_as_uint(mx) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
+          const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
+          if (piece8 == 0) sh.qs[half][col] = 1.4426950408889634f * rsqrtf((float)D) * __uint_as_float((uint32_t)(127 - up) << 23);
+          for (uint32_t* e : {&w.x, &w.y, &w.z, &w.w}) {
+            const float2 x = qc_elems(*e, a.f16);
+            const __half2 h = __floats2half2_rn(x.x * mul, x.y * mul);
+            *e = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place(col)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+        }
+        fence_proxy_async();
         __syncwarp();
         qs = sh.qs[half][t128];
-        fence_proxy_async();
       }
       __syncwarp();
       if (lane == 0 && p.n_steps > 0) qp_arrive(&sh.q_full[half]);
@@ -584,7 +587,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           }
         }
         __syncwarp();
-#pragma unroll 2
+#pragma unroll 1
         for (int i = 0; i < PIECES; ++i) {              // 32 pieces a time
           const int col = i * (32 / PIECES) + lane / PIECES, pc = lane % PIECES, cc = (warp & 3) * 32 + col;
           uint4 w;
@@ -595,7 +598,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             to[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
             to[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
           } else {
-            uint8_t* to = static_cast<uint8_t*>(a.out) + ((size_t)(u.row0 + cc / a.G) * a.Hq + u.h * a.G + cc % a.G) * D * (wide ? 4 : 2);
+            uint8_t* to = static_cast<uint8_t*>(a.out) + qt_query(a, u, cc) * D * (wide ? 4 : 2);
             *reinterpret_cast<uint4*>(to + round * (2 * D) + pc * 16) = w;
           }
         }
