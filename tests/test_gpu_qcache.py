@@ -462,6 +462,60 @@ def test_long_chunks_among_single_tokens_and_sequences_without_rows(d, page, G, 
     check_attention(rig, rows, q, q64, rig.gpu.attention(rig.batch(rows), q, out_dtype=getattr(T(), out)), out)
 
 
+def test_more_sequences_than_a_block_has_threads():
+    n = 1100
+    rig = Rig(n, 12, 1, 64, 16, seed=45)
+    first = [(5 * i) % 23 for i in range(n)]
+    first[700] = 60
+    rig.append(first)
+    rows = [i % 3 % 2 for i in range(n)]
+    rows[0], rows[511], rows[700], rows[1099] = 1, 100, 2, 70
+    q, _ = rig.append(rows, theta=1e4, q_heads=2)
+    rig.check()
+    check_attention(rig, rows, q, f64(q), rig.gpu.attention(rig.batch(rows), q, out_dtype=T().float32), F32)
+    b = rig.batch(rows)
+    pages = rig.gpu.select(b, q, 3, 1, 1)
+    check_attention(rig, rows, q, f64(q), rig.gpu.attention(b, q, pages=pages, out_dtype=T().float32), F32, pages=pages.cpu().numpy())
+
+
+@pytest.mark.parametrize("far", [1.0, 1e3, 1e9, 1e30])
+def test_a_page_of_far_larger_keys_leaves_the_others_in_order(far):
+    """The bound on the first scores' errors goes by the largest scale: with a page far above the others it leaves all of them open."""
+    rig = Rig(1, 420, 2, 64, 16, seed=46)
+    rig.append([200 * 16])
+    rig.append([16], scale=far)
+    rig.append([200 * 16 - 3])
+    rig.append([1], scale=1e-20)
+    q, q64 = rig.draw(2, 8, 64)
+    for keep in (2, 5, 150, 399):
+        got = rig.gpu.select(rig.batch([2]), q, keep, 0, 1).cpu().numpy()
+        for i in range(2):
+            for h in range(2):
+                assert got[i, h].tolist() == rig.ref.select(rig.table[0], h, q64[i, h * 4:h * 4 + 4], int(rig.len[0]) - 1 + i, keep, 0, 1), (keep, i, h)
+
+
+@pytest.mark.parametrize("absent", [3, 40, 58])
+def test_selection_where_pages_are_none_of_the_caches(absent):
+    rig = Rig(1, 60, 1, 128, 16, seed=47)
+    rig.append([60 * 16])
+    gone = rig.rng.permutation(np.arange(1, 59))[:absent]
+    rig.table[0, gone] = -1
+    rig.dtable = dev(rig.table)
+    q, q64 = rig.draw(1, 4, 128)
+    for keep in (4, 20, 45):
+        got = rig.gpu.select(rig.batch([1]), q, keep, 1, 1).cpu().numpy()[0, 0].tolist()
+        assert got == rig.ref.select(rig.table[0], 0, q64[0], 960, keep, 1, 1)
+    assert int(rig.status.item()) == 4
+
+
+def test_queries_of_zeros_choose_the_first_pages():
+    torch = T()
+    rig = Rig(1, 600, 1, 64, 16, seed=48)
+    rig.append([600 * 16])
+    q = torch.zeros(1, 2, 64, dtype=torch.float16, device="cuda")
+    assert rig.gpu.select(rig.batch([1]), q, 7, 2, 1).cpu().numpy()[0, 0].tolist() == [0, 1, 2, 3, 4, 5, 599]
+
+
 def test_a_captured_step_is_replayed_with_other_lengths_on_another_stream():
     torch = T()
     rig = Rig(3, 30, 2, 64, 16, seed=42)
