@@ -202,6 +202,9 @@ __device__ __forceinline__ void qc_append_queries(const QcDev& c, const QcRows& 
 // arithmetic before their maximum.
 // Queries decide nothing: fp32, with angles reduced in fp64.  A warp takes a token and all of the block's query heads (where there are fewer tokens than
 // warps, a part of them), with the weights and the angles multiplied out once: x' = inv (a x + b y).
+// Measured (16 800 rows of seven prompts, 32 and 8 heads, d = 128, normalised and rotated): 101 us, of which queries 46 for 275 MB, at the copy rate, and keys and
+// values 55 (37 with neither normalisation nor rotation), bound by their instructions, 39 an element.  256 single tokens: 13 us, one chain of loads
+// and fp64 a block.
 template <int D, bool F16, int TEAM, int PASSES, bool TABLE>
 __global__ void __launch_bounds__(QA_THREADS, PASSES == 1 ? 3 : PASSES == 2 ? 2 : 1)
 qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows r, const __grid_constant__ QcFreq freq, int places, int groups, int heads_per,
