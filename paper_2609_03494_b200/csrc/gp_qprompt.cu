@@ -207,7 +207,10 @@ struct QpWalk {
 // the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
 // sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
 // keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
-// What bounds it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with d = 128 the same.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 250 us, 660 TFLOP/s.
+// What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
+// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2300 cycles for two
+// warps a scheduler; and 25 000 cycles between two units.
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
 qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
