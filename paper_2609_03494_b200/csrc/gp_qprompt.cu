@@ -207,9 +207,9 @@ struct QpWalk {
 // the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
 // sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
 // keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
-// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 250 us, 660 TFLOP/s.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 234 us, 705 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
-// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2300 cycles for two
+// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2150 cycles for two
 // warps a scheduler; and 25 000 cycles between two units.
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
@@ -392,6 +392,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       u.cols = u.rows * a.G;
       const bool used = u.cols > 0, real = t128 < u.cols;
       const int see = real ? qt_visible(c, a, u, t128) : 0x7fffffff;
+      const int least = __reduce_min_sync(0xffffffffu, see);
       float qs = 0.f;                                   // what S is multiplied with
       if (used && p.n_steps > 0) {                      // the warp's 32 columns, D / 8 lanes a column
         constexpr int LPC = D / 8, CPR = 32 / LPC, ROUNDS = 32 / CPR;
@@ -442,20 +443,16 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         qp_fence_after();
         if (used) {
           const uint32_t t_x = t_s + (s & 1) * 64;
-          float x0[32], x1[32];
-          qp_ld32(t_x, x0);
-          qp_ld32(t_x + 32, x1);
           const float4 kq = *reinterpret_cast<const float4*>(sh.ks[slot]), eq = *reinterpret_cast<const float4*>(sh.ev[slot]);
+          const int t0 = u.t0 + j * QP_N;
+          int masked = t0 + QP_N > least || fminf(fminf(kq.x, kq.y), fminf(kq.z, kq.w)) < 0.f;      // some row does not see all of the step
           const float ks[4] = {kq.x, kq.y, kq.z, kq.w};
           float ev[4] = {eq.x, eq.y, eq.z, eq.w};
-          const int t0 = u.t0 + j * QP_N;
           float top = -1000.f, f[4];
-          bool gone = false;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             f[g] = fmaxf(ks[g] * qs, 1.2e-38f);
-            if (ks[g] < 0.f) gone = true;
-            else top = fmaxf(top, ev[g]);
+            if (ks[g] >= 0.f) top = fmaxf(top, ev[g]);
           }
           // E, and the exponents as far as they matter beside it: values 2^100 below E's (a page of zeros has the smallest exponent there is) may count as
           // 2^-100 times E's, their weights count alike
@@ -466,14 +463,26 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           }
 #pragma unroll
           for (int g = 0; g < 4; ++g) ev[g] = fmaxf(ev[g], E - 100.f);
-          const bool masked = __any_sync(0xffffffffu, t0 + QP_N > see) || gone;      // some row does not see all of the step
-          qp_wait_ld();
-          if (masked) {
+          float x0[32], x1[32];
+#pragma unroll 1
+          for (;;) {
+            qp_ld32(t_x, x0);
+            qp_ld32(t_x + 32, x1);
+            qp_wait_ld();
+            if (!masked) break;
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {               // -infinity where a row does not see a token, in tensor memory: two forms of x would cost 64 moves a step
+              float x[16];
+              qp_ld16(t_x + g * 16, x);
+              qp_wait_ld();
+              const int left = sh.ks[slot][g] < 0.f ? 0 : see - t0 - g * 16;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              x0[e] = t0 + e < see && ks[e >> 4] >= 0.f ? x0[e] : -INFINITY;
-              x1[e] = t0 + 32 + e < see && ks[2 + (e >> 4)] >= 0.f ? x1[e] : -INFINITY;
+              for (int e = 0; e < 16; ++e) x[e] = e < left ? x[e] : -INFINITY;
+              qp_st16(t_x + g * 16, reinterpret_cast<const uint32_t*>(x));
             }
+            qp_wait_st();
+            masked = 0;
+            asm volatile("" : "+r"(masked));            // (or the compiler makes two of it)
           }
           float mx = -INFINITY;                         // the largest s + ev of the step
 #pragma unroll
