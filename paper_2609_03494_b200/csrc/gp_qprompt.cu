@@ -331,11 +331,13 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         const bool all = first + QP_N <= u.t1 && __all_sync(0xffffffffu, ids >= 0 || lane >= QP_N / 16);
         const int slot0 = first & (c.page - 1);
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-          const int t = i * TPI + tt;
-          const int id = __shfl_sync(0xffffffffu, ids, i * TPI / 16);
-          const uint4* from = reinterpret_cast<const uint4*>(src + (size_t)max(id, 0) * page_bytes + ((slot0 + t) & (c.page - 1)) * D);
-          r[i] = all || (id >= 0 && first + t < u.t1) ? __ldg(from) : make_uint4(0, 0, 0, 0);
+        for (int g = 0; g < QP_N / 16; ++g) {           // (a step's groups of 16 tokens lie in one page each)
+          const int id = __shfl_sync(0xffffffffu, ids, g);
+          const uint8_t* from = src + (size_t)max(id, 0) * page_bytes + (((slot0 + g * 16) & (c.page - 1)) + tt) * D;
+          const int left = all ? 16 : id >= 0 ? u.t1 - first - g * 16 - tt : 0;
+#pragma unroll
+          for (int i = 0; i < 16 / TPI; ++i)
+            r[g * (16 / TPI) + i] = i * TPI < left ? __ldg(reinterpret_cast<const uint4*>(from + i * TPI * D)) : make_uint4(0, 0, 0, 0);
         }
         sc = make_float2(-1.f, 1.f);
         if (!kv && ids >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((size_t)ids * c.Hkv + u.h) * 2);
