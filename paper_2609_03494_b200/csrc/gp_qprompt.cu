@@ -1,6 +1,8 @@
 // Attention over the 8-bit cache for many rows of a sequence at once (chunks of prompts): both products on the fifth-generation tensor cores.
 #include "gp_qprompt.cuh"
 
+#include <utility>
+
 namespace {
 
 constexpr int QP_M = 128;                      // columns (row, query head of the group) of a half of a block's tile: the rows of a product
@@ -48,6 +50,15 @@ __device__ __forceinline__ void qp_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void qp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void qp_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void qp_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+template <int AT>
+__device__ __forceinline__ void qp_store16(uint32_t to, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0 + %5], {%1, %2, %3, %4};" ::"r"(to), "r"(x), "r"(y), "r"(z), "r"(w), "n"(AT) : "memory");
+}
+// f(0) .. f(N - 1), each number a constant
+template <class F, int... I>
+__device__ __forceinline__ void qp_each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void qp_each(F&& f) { qp_each_of(f, std::make_integer_sequence<int, N>{}); }
 // 32, 16, 8 columns of the warp's 32 lanes
 __device__ __forceinline__ void qp_ld32(uint32_t t, float* x) {
   uint32_t* r = reinterpret_cast<uint32_t*>(x);
@@ -360,17 +371,14 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
                     __vcmpeq4(r[i].w & 0x7f7f7f7f, 0x7f7f7f7f)) != 0;
           if (nan) *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) = piece;
         }
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
+        const uint32_t to = dst + at * OPERAND, to0 = to + at0, to1 = to + at1, odd0 = to + (at0 ^ 64), odd1 = to + (at1 ^ 64);
+        qp_each<IT>([&](auto no) {
+          constexpr int i = decltype(no)::value;
           const uint32_t xa = flip ? r[i].z : r[i].x, ya = flip ? r[i].w : r[i].y, xb = flip ? r[i].x : r[i].z, yb = flip ? r[i].y : r[i].w;
-          const uint32_t row = dst + at * OPERAND + i * TPI * 128, odd = TPI == 4 ? (i & 1) << 6 : 0;      // (token & 7 goes by the round too)
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (at0 ^ odd)), "r"(e4m3x2_to_f16x2(xa)), "r"(e4m3x2_hi_to_f16x2(xa)),
-                       "r"(e4m3x2_to_f16x2(ya)), "r"(e4m3x2_hi_to_f16x2(ya))
-                       : "memory");
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (at1 ^ odd)), "r"(e4m3x2_to_f16x2(xb)), "r"(e4m3x2_hi_to_f16x2(xb)),
-                       "r"(e4m3x2_to_f16x2(yb)), "r"(e4m3x2_hi_to_f16x2(yb))
-                       : "memory");
-        }
+          constexpr bool odd = TPI == 4 && (i & 1);     // (token & 7 goes by the round too)
+          qp_store16<i * TPI * 128>(odd ? odd0 : to0, e4m3x2_to_f16x2(xa), e4m3x2_hi_to_f16x2(xa), e4m3x2_to_f16x2(ya), e4m3x2_hi_to_f16x2(ya));
+          qp_store16<i * TPI * 128>(odd ? odd1 : to1, e4m3x2_to_f16x2(xb), e4m3x2_hi_to_f16x2(xb), e4m3x2_to_f16x2(yb), e4m3x2_hi_to_f16x2(yb));
+        });
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
