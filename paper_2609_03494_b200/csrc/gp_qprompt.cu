@@ -8,6 +8,7 @@ namespace {
 constexpr int QP_M = 128;                      // columns (row, query head of the group) of a half of a block's tile: the rows of a product
 constexpr int QP_COLS = 2 * QP_M;
 constexpr int QP_N = 64;                       // tokens of a step
+constexpr long long QP_PATIENCE = 1ll << 32;   // cycles (2 s) after which a wait gives up
 constexpr int QP_RING = 4;                     // steps whose keys and values there is room for
 constexpr int QP_SOFT = 256;                   // threads that turn logits into weights, a column each (warps 0 .. 7)
 constexpr int QP_TURN = 3;                     // warps that turn keys into fp16, a step each in turn (8 .. 10); as many turn values (11 .. 13)
@@ -59,6 +60,11 @@ template <class F, int... I>
 __device__ __forceinline__ void qp_each_of(F&& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 template <int N, class F>
 __device__ __forceinline__ void qp_each(F&& f) { qp_each_of(f, std::make_integer_sequence<int, N>{}); }
+// The two warps of weights of a scheduler (one of each half) take turns at the exponentials, so that one's wait, logits and maximum fall into the other's
+// turn; left to themselves they run in step or not by chance (chunks of 32 768 tokens 608 to 657 us; 579 so).  Both make a turn of each step of a piece
+// whether the half is used or not, and all their other waits are bounded: every turn comes.
+__device__ __forceinline__ void qp_turn(int id) { __syncwarp(); asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void qp_pass(int id) { __syncwarp(); asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
 // 32, 16, 8 columns of the warp's 32 lanes
 __device__ __forceinline__ void qp_ld32(uint32_t t, float* x) {
   uint32_t* r = reinterpret_cast<uint32_t*>(x);
@@ -97,10 +103,24 @@ struct QpShared {
   long long x1, share, upto[QP_THREADS], warp[QP_THREADS / 32];
   float plain[2][QT_WARPS * 130], qs[2][QP_M];
 };
-// A bounded wait for a phase of a barrier.
+// A bounded wait for a phase of a barrier.  (Without a time to suspend for, which brings a second look and a timer to each try: 627 -> 608 us.)
+__device__ __forceinline__ bool qp_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ void qp_wait(QpShared& sh, uint64_t* bar, uint32_t parity) {
-  for (unsigned spin = 0; !mbar_try_wait(bar, parity); ++spin)
-    if (spin > GP_SPIN_LIMIT || *reinterpret_cast<volatile int*>(&sh.dead)) { *reinterpret_cast<volatile int*>(&sh.dead) = 1; break; }
+  const uint32_t at = smem_u32(bar);
+  if (qp_try(at, parity)) return;
+  const long long since = clock64();
+  while (!qp_try(at, parity))
+    if (clock64() - since > QP_PATIENCE || *reinterpret_cast<volatile int*>(&sh.dead)) { *reinterpret_cast<volatile int*>(&sh.dead) = 1; break; }
 }
 
 // The line of work (as in the other kernel): sequence by sequence, KV head by KV head, tile of rows by tile of rows, measured in tokens.  Tile t of
@@ -218,9 +238,9 @@ struct QpWalk {
 // the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
 // sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
 // keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
-// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 234 us, 705 TFLOP/s.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 211 us, 780 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
-// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2150 cycles for two
+// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2000 cycles for two
 // warps a scheduler; and 25 000 cycles between two units.
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
@@ -394,6 +414,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     const int half = warp >> 2, t128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + T_S + half * 128, t_o = tmem + lanes + T_O + half * 128;
+    const int turn = 3 + (warp & 3) * 2;              // barriers 3 .. 10 (qt_plain has 1 and 2)
+    if (half) qp_pass(turn);
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       QtUnit u = p.u;                                   // of this half
@@ -530,6 +552,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             }
           }
           const float zero = M == -INFINITY ? 0.f : M;
+          qp_turn(turn + half);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {                 // weights of 16 columns to tensor memory
             const float* x = (g & 2 ? x1 : x0) + (g & 1) * 16;
@@ -556,7 +579,11 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             qp_st8(t_x + g * 8, hi);
             if (TERMS == 2) qp_st8(t_x + 32 + g * 8, lo);
           }
+          qp_pass(turn + 1 - half);
           qp_wait_st();
+        } else {
+          qp_turn(turn + half);
+          qp_pass(turn + 1 - half);
         }
         qp_fence_before();
         __syncwarp();
@@ -630,6 +657,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       if (p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece)      // some row may have met another's NaN: all of the half in plain arithmetic
         qt_plain<D>(c, a, u, sh.plain[half], parts, 1 + half);
     }
+    if (!half) qp_turn(turn);
   }
   qp_fence_before();
   __syncthreads();
