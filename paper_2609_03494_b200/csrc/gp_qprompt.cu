@@ -14,7 +14,8 @@ constexpr int QP_SOFT = 256;                   // threads that turn logits into 
 constexpr int QP_TURN = 3;                     // warps that turn keys into fp16, a step each in turn (8 .. 10); as many turn values (11 .. 13)
 constexpr int QP_ISSUER = 14;                  // the first of the two warps that issue the products, one for each half
 constexpr int QP_THREADS = QP_SOFT + (2 * QP_TURN + 2) * 32;
-constexpr int QP_UNIT = 256;                   // what a unit costs beside its tokens, in tokens
+constexpr int QP_UNIT = 640;                   // what a unit costs beside its tokens, in tokens (chunks with 256 / 512 / 640 / 768 / 1024: 204 / 198 / 196 / 195 / 196 us;
+                                               // six sequences of 100 to 700 rows: 202 / 158 / 146 / 146 / 150)
 constexpr float QP_SLACK = 7.f;                // a row's maximum is brought up to date when something passes it by 2^7
 constexpr float QP_LIFT = 8.f;
 constexpr int QP_QBLOCK = QP_M * 128;          // bytes of 64 fp16 channels of the queries of a half
@@ -238,10 +239,10 @@ struct QpWalk {
 // the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
 // sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
 // keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
-// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 211 us, 780 TFLOP/s.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 195 us, 845 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
-// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2000 cycles for two
-// warps a scheduler; and 25 000 cycles between two units.
+// d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2100 cycles for two
+// warps a scheduler; and 20 000 cycles between two units.
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
 qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
@@ -442,23 +443,35 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         cp_async_wait<0>();
         __syncwarp();
         col -= ROUNDS * CPR;
+        const float root = 1.4426950408889634f * rsqrtf((float)D);
 #pragma unroll 1
-        for (int i = 0; i < ROUNDS; ++i, col += CPR) {
-          uint4 w;
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place(col)));
-          float mx = 0.f;
-          for (uint32_t e : {w.x, w.y, w.z, w.w}) { const float2 x = qc_elems(e, a.f16); mx = fmaxf(mx, fmaxf(fabsf(x.x), fabsf(x.y))); }
+        for (int i = 0; i < ROUNDS; i += 4, col += 4 * CPR) {      // four at once: a chain of 400 cycles
+          uint4 w[4];
+          float mx[4];
 #pragma unroll
-          for (int o = 1; o < LPC; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-          const int ex = max((int)(__float_as_uint(mx) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
-          const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
-          if (piece8 == 0) sh.qs[half][col] = 1.4426950408889634f * rsqrtf((float)D) * __uint_as_float((uint32_t)(127 - up) << 23);
-          for (uint32_t* e : {&w.x, &w.y, &w.z, &w.w}) {
-            const float2 x = qc_elems(*e, a.f16);
-            const __half2 h = __floats2half2_rn(x.x * mul, x.y * mul);
-            *e = *reinterpret_cast<const uint32_t*>(&h);
+          for (int k = 0; k < 4; ++k)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[k].x), "=r"(w[k].y), "=r"(w[k].z), "=r"(w[k].w) : "r"(place(col + k * CPR)));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            mx[k] = 0.f;
+            for (uint32_t e : {w[k].x, w[k].y, w[k].z, w[k].w}) { const float2 x = qc_elems(e, a.f16); mx[k] = fmaxf(mx[k], fmaxf(fabsf(x.x), fabsf(x.y))); }
           }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place(col)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+#pragma unroll
+          for (int o = 1; o < LPC; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], o));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int ex = max((int)(__float_as_uint(mx[k]) >> 23) - 127, -100), up = min(14 - ex, 114);    // largest magnitude to 2^14 .. 2^15, as in the other kernel
+            const float mul = __uint_as_float((uint32_t)(127 + up) << 23);
+            if (piece8 == 0) sh.qs[half][col + k * CPR] = root * __uint_as_float((uint32_t)(127 - up) << 23);
+            for (uint32_t* e : {&w[k].x, &w[k].y, &w[k].z, &w[k].w}) {
+              const float2 x = qc_elems(*e, a.f16);
+              const __half2 h = __floats2half2_rn(x.x * mul, x.y * mul);
+              *e = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(place(col + k * CPR)), "r"(w[k].x), "r"(w[k].y), "r"(w[k].z), "r"(w[k].w) : "memory");
+          }
         }
         fence_proxy_async();
         __syncwarp();
@@ -637,18 +650,25 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         }
         __syncwarp();
 #pragma unroll 1
-        for (int i = 0; i < PIECES; ++i) {              // 32 pieces a time
-          const int col = i * (32 / PIECES) + lane / PIECES, pc = lane % PIECES, cc = (warp & 3) * 32 + col;
-          uint4 w;
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place(col, pc)));
-          if (cc >= u.cols) continue;
-          if (parts) {
-            float2* to = reinterpret_cast<float2*>(parts + (size_t)cc * ST + round * (D / 2) + pc * 4);
-            to[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
-            to[1] = make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
-          } else {
-            uint8_t* to = static_cast<uint8_t*>(a.out) + qt_query(a, u, cc) * D * (wide ? 4 : 2);
-            *reinterpret_cast<uint4*>(to + round * (2 * D) + pc * 16) = w;
+        for (int i = 0; i < PIECES; i += 4) {           // 32 pieces a time
+          const int pc = lane % PIECES;
+          uint4 w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[k].x), "=r"(w[k].y), "=r"(w[k].z), "=r"(w[k].w)
+                         : "r"(place((i + k) * (32 / PIECES) + lane / PIECES, pc)));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int cc = (warp & 3) * 32 + (i + k) * (32 / PIECES) + lane / PIECES;
+            if (cc >= u.cols) continue;
+            if (parts) {
+              float2* to = reinterpret_cast<float2*>(parts + (size_t)cc * ST + round * (D / 2) + pc * 4);
+              to[0] = make_float2(__uint_as_float(w[k].x), __uint_as_float(w[k].y));
+              to[1] = make_float2(__uint_as_float(w[k].z), __uint_as_float(w[k].w));
+            } else {
+              uint8_t* to = static_cast<uint8_t*>(a.out) + qt_query(a, u, cc) * D * (wide ? 4 : 2);
+              *reinterpret_cast<uint4*>(to + round * (2 * D) + pc * 16) = w[k];
+            }
           }
         }
         __syncwarp();
