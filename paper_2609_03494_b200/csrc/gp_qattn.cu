@@ -467,8 +467,8 @@ QtPlan qt_plan(const QcDev& c, int G, int d, int n_list, bool list) {
   const int rows = list ? 1 : all ? c.max_rows : qt_few(d) / G;
   const long long cols = (long long)rows * G;
   // Tiles of columns by what a sequence may have; beside sequences of many rows most have one row (255 of them beside one of 2048 rows: 272 us with single
-  // tiles, 380 with as many as 48 columns want).  (Four tiles of 128 elements do not fit the registers.)
-  p.nt = cols <= 8 || !all ? 1 : cols <= 16 ? 2 : cols <= 24 || d == 128 ? 3 : 4;
+  // tiles, 380 with as many as 48 columns want).
+  p.nt = cols <= 8 || !all ? 1 : cols <= 16 ? 2 : cols <= 24 ? 3 : 4;
   if (list) p.nt = 1;
   const int rows_tile = list ? 1 : p.nt * 8 / G;
   const long long units = (long long)c.n_seq * ((list ? c.max_rows : rows) + rows_tile - 1) / rows_tile * c.Hkv;

@@ -6,9 +6,10 @@ constexpr int QT_WARPS = 4;
 constexpr int QT_THREADS = QT_WARPS * 32;
 
 // A sequence goes to the kernel for few rows (gp_qattn.cu) up to this many columns (row, query head of the group), beyond it to the one for many
-// (gp_qprompt.cu), whose tiles have 256.  16 sequences of 3000 tokens, 8 KV heads, us: d = 64 with 48 / 64 / 96 columns 57 / 60 / 84 in the former, 63 / 64 /
-// 65 in the latter; d = 128 with 32 / 48 / 64 columns 75 / 80 / 109 and 90 / 91 / 91.
-constexpr int qt_few(int d) { return d == 64 ? 64 : 48; }
+// (gp_qprompt.cu), whose tiles have 256.  3000 tokens, 8 KV heads, us: d = 64, 16 sequences, with 32 / 48 / 64 columns 39 / 55 / 57 in the former, 60 in
+// the latter (64 sequences: 103 / 179 / 187 and 177; one of 12 000 tokens: 29 and 34); d = 128 with 16 / 24 / 32 / 48 columns 38 / 52 / 75 / 78 and
+// 68 / 69 / 70 / 71 (64 sequences: 95 / 139 / 246 / 256 and 202; one: 25 / 30 / 34 / 34 and 36).
+constexpr int qt_few(int d) { return d == 64 ? 64 : 24; }
 
 struct QtArgs {
   const unsigned short* q;
