@@ -596,3 +596,48 @@ def test_the_holder_refuses_what_the_kernels_could_not_read():
         B.QBatch(torch.zeros(2, device="cuda"), rig.dtable[0], rig.dtable, 1, 1, 1)
     with pytest.raises(ValueError):
         B.QCache(rig.codes.view(torch.uint8), rig.scales)
+
+
+@pytest.mark.parametrize("d,G,rows", [(128, 4, 6), (128, 4, 7), (128, 8, 3), (128, 8, 4), (64, 4, 16), (64, 4, 17), (64, 8, 8), (64, 8, 9)])
+def test_attention_at_the_border_between_few_and_many_rows(d, G, rows):
+    rig = Rig(3, 20, 2, d, 16, seed=70 + rows)
+    rig.append([rows, 200, 97])
+    q, q64 = rig.draw(3 * rows, 2 * G, d)
+    for out in (BF16, F32):
+        check_attention(rig, [rows] * 3, q, q64, rig.gpu.attention(rig.batch([rows] * 3), q, out_dtype=getattr(T(), out)), out)
+
+
+@pytest.mark.parametrize("d,G,out", [(128, 4, BF16), (64, 8, F32)])
+@pytest.mark.parametrize("rows", [30, 150])
+def test_many_rows_where_pages_are_none_of_the_caches(d, G, out, rows):
+    """A page that is not there counts as not seen, wherever in a step it lies; all of a step, too."""
+    rig = Rig(2, 40, 1, d, 16, seed=80 + rows)
+    rig.append([40 * 16 - 5, 300])
+    gone = [[0, 5, 8, 9, 10, 11, 21, 30, 31, 39], [2, 18]]
+    q, q64 = rig.draw(2 * rows, G, d)
+    held = np.full((2 * rows, 1, 40), -1)
+    for s in range(2):
+        rig.table[s, gone[s]] = [-1, 1 << 30] * (len(gone[s]) // 2)
+        held[s * rows:(s + 1) * rows, 0, :] = [-1 if p in gone[s] else p for p in range(40)]
+    rig.dtable = dev(rig.table)
+    got = rig.gpu.attention(rig.batch([rows] * 2), q, out_dtype=getattr(T(), out))
+    check_attention(rig, [rows] * 2, q, q64, got, out, held)
+    assert int(rig.status.item()) == 4
+
+
+def test_many_rows_of_many_short_sequences_and_of_half_tiles():
+    """Several pieces a block, most of them with nothing in the tile's second half, some of one step."""
+    rig = Rig(60, 16, 8, 128, 16, seed=90)
+    rng = np.random.default_rng(1)
+    rig.append(list(rng.integers(40, 250, 60)))
+    rows = [int(min(r, n)) for r, n in zip(rng.integers(7, 90, 60), rig.len)]
+    q, q64 = rig.draw(sum(rows), 32, 128)
+    got = f64(rig.gpu.attention(rig.batch(rows), q, out_dtype=T().float32))
+    # some of the sequences
+    at = np.concatenate([[0], np.cumsum(rows)])
+    for s in (0, 17, 59):
+        one = Rig.__new__(Rig)
+        one.__dict__.update(rig.__dict__)
+        one.table, one.dtable, one.len = rig.table[s:s + 1], dev(rig.table[s:s + 1]), rig.len[s:s + 1]
+        part = slice(at[s], at[s + 1])
+        check_attention(one, [rows[s]], q[part], q64[part], dev(got[part].astype(np.float32)), F32)
