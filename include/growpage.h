@@ -472,6 +472,9 @@ int gp_attention_noalloc(const void* q, const void* k, const void* v, const int3
  * are infinite or not numbers are held as NaN and do not count for the scale; magnitudes above 448 * 2^119 as that.
  * `bounds`, needed by gp_qcache_select only, has per (page, KV head) the smallest and the largest code of every
  * channel of the keys held there (a NaN counts as 0).
+ * A sequence may become shorter: rows behind its new end (drafts that were not taken) are replaced by the next rows that are
+ * appended there.  That append takes the page's bounds from the rows that are held then; a scale keeps the size of what
+ * was ever put into the page since its first row was, i.e. it never shrinks while the page holds a row.
  * Pages may be shared between sequences as long as they are full. */
 typedef struct gp_qcache {
   int32_t  n_kv_heads;

@@ -203,8 +203,8 @@ __device__ __forceinline__ void qc_append_queries(const QcDev& c, const QcRows& 
 // Queries decide nothing: fp32, with angles reduced in fp64.  A warp takes a token and all of the block's query heads (where there are fewer tokens than
 // warps, a part of them), with the weights and the angles multiplied out once: x' = inv (a x + b y).
 // Measured (16 800 rows of seven prompts, 32 and 8 heads, d = 128, normalised and rotated): 101 us, of which queries 46 for 275 MB, at the copy rate, and keys and
-// values 55 (37 with neither normalisation nor rotation), bound by their instructions, 39 an element.  256 single tokens: 13 us, one chain of loads
-// and fp64 a block.
+// values 55 (37 with neither normalisation nor rotation), bound by their instructions, 39 an element.  256 single tokens, pages of 16 / 64 / 256: 9.9 / 12.0 /
+// 27.8 us, one chain of loads and fp64 a block, and the keys that a page holds read for its bounds (2 / 8 / 33 MB).
 template <int D, bool F16, int TEAM, int PASSES, bool TABLE>
 __global__ void __launch_bounds__(QA_THREADS, PASSES == 1 ? 3 : PASSES == 2 ? 2 : 1)
 qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows r, const __grid_constant__ QcFreq freq, int places, int groups, int heads_per,
@@ -274,7 +274,11 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
   for (int h = h0 + team; h < h1; h += TEAMS) {
     const size_t unit = (size_t)pid * c.Hkv + h;
     float2 old_scale = make_float2(1.f, 1.f);
-    if (kept) old_scale = *reinterpret_cast<const float2*>(c.scales + unit * 2);
+    if (kept) {
+      old_scale = *reinterpret_cast<const float2*>(c.scales + unit * 2);
+      if (c.bounds)                                   // keys that are there already: wanted for the bounds, behind this head's arithmetic
+        if (tw == 0 && lane == 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(c.codes + unit * 2 * c.page * D), "r"(kept * D) : "memory");
+    }
     auto key_rows = [&](int u, int t, double* y) {    // a row's part, normalised and rotated
       float f[16];
       qc_elems8<F16>(kraw[u][0], f);
@@ -379,6 +383,23 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
     uint32_t lo[8], hi[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) { lo[e] = PINF2; hi[e] = NINF2; }
+    auto bound = [&](int e, uint32_t w) {
+      lo[e] = u2(__hmin2(h2(lo[e]), h2(w)));
+      hi[e] = u2(__hmax2(h2(hi[e]), h2(w)));
+    };
+    auto numbers = [&](uint32_t w) { return w & __heq2_mask(h2(w), h2(w)); };      // NaN counts as 0
+    if (c.bounds && kept) {                           // rows that are there already, from their codes: the old bounds may hold rows that were taken back since
+      if (ek != ek0) team_sync();
+#pragma unroll 4
+      for (int t = tw * RPW + sub; t < kept; t += TEAM * RPW) {
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const uint2 w = *reinterpret_cast<const uint2*>(kdst + (size_t)t * D + lr * 8 + hf * HALF);
+          bound(hf * 4, numbers(e4m3x2_to_f16x2(w.x))); bound(hf * 4 + 1, numbers(e4m3x2_hi_to_f16x2(w.x)));
+          bound(hf * 4 + 2, numbers(e4m3x2_to_f16x2(w.y))); bound(hf * 4 + 3, numbers(e4m3x2_hi_to_f16x2(w.y)));
+        }
+      }
+    }
     const float km = pow2f(-ek), vm = pow2f(-ev);
 #pragma unroll
     for (int u = 0; u < PASSES; ++u) {
@@ -399,11 +420,7 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
           *reinterpret_cast<uint2*>(kdst + off + hf * HALF) = w;
           const uint32_t num[4] = {e4m3x2_to_f16x2(w.x), e4m3x2_hi_to_f16x2(w.x), e4m3x2_to_f16x2(w.y), e4m3x2_hi_to_f16x2(w.y)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t v = odd ? num[e] & __heq2_mask(h2(num[e]), h2(num[e])) : num[e];      // NaN counts as 0
-            lo[hf * 4 + e] = u2(__hmin2(h2(lo[hf * 4 + e]), h2(v)));
-            hi[hf * 4 + e] = u2(__hmax2(h2(hi[hf * 4 + e]), h2(v)));
-          }
+          for (int e = 0; e < 4; ++e) bound(hf * 4 + e, odd ? numbers(num[e]) : num[e]);
           float g[8];
           qc_elems8<F16>(vraw[u][hf], g);
           if (odd) {
@@ -458,20 +475,8 @@ qc_append_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QcRows
         for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            uint32_t* dst = reinterpret_cast<uint32_t*>(b + side * D + hf * HALF) + e;
-            uint32_t w0 = side ? hi[hf * 4 + e * 2] : lo[hf * 4 + e * 2], w1 = side ? hi[hf * 4 + e * 2 + 1] : lo[hf * 4 + e * 2 + 1];
-            if (kept) {                               // bounds of the rows that were there, in the new scale
-              uint32_t o = *dst;
-              if (ek != ek0) {
-                const float m = pow2f(ek0 - ek);
-                const float2 l2 = qc_half2(e4m3x2_to_f16x2(o)), g2 = qc_half2(e4m3x2_hi_to_f16x2(o));
-                o = qc_codes(l2.x * m, l2.y * m, g2.x * m, g2.y * m);
-              }
-              const __half2 o0 = h2(e4m3x2_to_f16x2(o)), o1 = h2(e4m3x2_hi_to_f16x2(o));
-              w0 = u2(side ? __hmax2(h2(w0), o0) : __hmin2(h2(w0), o0));
-              w1 = u2(side ? __hmax2(h2(w1), o1) : __hmin2(h2(w1), o1));
-            }
-            *dst = f16x4_to_e4m3x4(w0, w1);
+            const uint32_t w0 = side ? hi[hf * 4 + e * 2] : lo[hf * 4 + e * 2], w1 = side ? hi[hf * 4 + e * 2 + 1] : lo[hf * 4 + e * 2 + 1];
+            reinterpret_cast<uint32_t*>(b + side * D + hf * HALF)[e] = f16x4_to_e4m3x4(w0, w1);
           }
     }
   }
@@ -899,9 +904,10 @@ int qc_append(const QcDev& c, const QcRows& r, const QcFreq& f, cudaStream_t s) 
   if (jobs > 4 * most) { jobs = most; places = 0; }
   if (q_jobs > 4 * q_most) { q_jobs = q_most; q_places = 0; }
   if (!r.q) q_jobs = 0;
-  // heads of a page together share the table of angles; apart where that leaves SMs without a block
+  // heads of a page together share the table of angles and keep a block's warps busy; apart where that leaves SMs without a block (256 single tokens, 8
+  // heads, pages of 16: 9.9 us; 12.1 with two blocks an SM, i.e. four heads a block)
   int heads_per = c.Hkv;
-  while (heads_per > 1 && jobs * ((c.Hkv + heads_per - 1) / heads_per) < 296) heads_per = (heads_per + 1) / 2;
+  while (heads_per > 1 && jobs * ((c.Hkv + heads_per - 1) / heads_per) < 148) heads_per = (heads_per + 1) / 2;
   const int groups = (c.Hkv + heads_per - 1) / heads_per;
   const long long kv = jobs * groups;
   int q_heads = r.Hq;
