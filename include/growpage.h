@@ -559,7 +559,8 @@ size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch,
  * the highest
  *     score = 2^e * sum over channels c of ( high_c * sum_g max(q_gc, 0) + low_c * sum_g min(q_gc, 0) ),
  * the sum over the group's query heads of the largest q.k that a key within the page's bounds can have; equal scores go
- * to the lower page.  fp64 throughout (integers come out of it).  NaN scores count as lowest.
+ * to the lower page.  fp64 throughout (integers come out of it).  NaN scores count as lowest (max(q, 0) and min(q, 0) of a NaN
+ * are 0; infinite queries can make scores NaN).
  *   pages   device int32 [n_rows][n_kv_heads][keep]: ascending, -1 behind the last
  * 1 <= recent, 0 <= first, first + recent <= keep.  q and work as for gp_qcache_attention (gp_qcache_select_bytes).  A page
  * whose id is none of the cache's has the lowest score. */

@@ -627,7 +627,8 @@ __device__ __forceinline__ unsigned long long qc_key(double x) {
   const unsigned long long b = (unsigned long long)__double_as_longlong(x + 0.0);
   return (b >> 63) ? ~b : b | 0x8000000000000000ull;
 }
-__device__ __forceinline__ uint32_t qc_key(float x) {
+__device__ __forceinline__ uint32_t qc_key(float x) {      // (as minus infinity)
+  if (!(x == x)) return 0x007fffffu;
   const uint32_t b = __float_as_uint(x + 0.f);
   return (b >> 31) ? ~b : b | 0x80000000u;
 }
@@ -770,8 +771,10 @@ qc_select_kernel(const __grid_constant__ QcDev c, const unsigned short* __restri
   int left = qs_descend<uint32_t>(sh, n, want, key, &thr, &known);
   // The want-th highest first score lies between the least and the greatest key with these bits; a page further than two errors from there is decided.
   const float far = 2.0001f * err;
-  // (keys of numbers, the infinite ones included, lie between these two)
-  const uint32_t above = qc_key(qc_unkey(min(thr | ~known, 0xff800000u)) + far), below = qc_key(qc_unkey(max(thr, 0x007fffffu)) - far);      // above: certain, below: certainly not
+  // (All keys lie between those of the two infinities.)  above: certain, below: certainly not.  Where a bound on the errors is not finite (the weights of a group's
+  // queries may pass what fp32 holds, and queries may be infinite) the first scores say nothing: all pages are close.
+  const bool told = far < INFINITY;
+  const uint32_t above = told ? qc_key(qc_unkey(min(thr | ~known, 0xff800000u)) + far) : ~0u, below = told ? qc_key(qc_unkey(max(thr, 0x007fffffu)) - far) : 0u;
   const int run = (n + QS_SEL_THREADS - 1) / QS_SEL_THREADS, i0 = min(tid * run, n), i1 = min(i0 + run, n);
   int gt = 0, eq = 0;
   for (int i = i0; i < i1; ++i) {

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_qcache import Rig
+from tests.test_gpu_qcache import Rig, T, dev, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,47 @@ def test_a_selection_after_drafts_were_taken_back_goes_by_the_keys_that_are_held
     got = rig.gpu.select(rig.batch([1]), q, 9, 1, 1).cpu().numpy()[0]
     for h in range(2):
         assert got[h].tolist() == rig.ref.select(rig.table[0], h, q64[0, 4 * h:4 * h + 4], n, 9, 1, 1)
+
+
+# ------------------------------------------------------------------------------------------------ selection at the ends of the range
+def guarded(rig, batch, q, rows, keep, first, recent):
+    """A selection into memory with other things on both sides of it."""
+    n = rows * rig.heads * keep
+    buf = T().full((n + 4096,), -77, dtype=T().int32, device="cuda")
+    rig.gpu.select(batch, q, keep, first, recent, pages=buf[2048:2048 + n].view(rows, rig.heads, keep))
+    got = buf.cpu().numpy()
+    assert (got[:2048] == -77).all() and (got[2048 + n:] == -77).all()
+    return got[2048:2048 + n].reshape(rows, rig.heads, keep)
+
+
+@pytest.mark.parametrize("d,heads", [(64, 2), (128, 1)])
+@pytest.mark.parametrize("pages", [100, 500])
+def test_selection_by_queries_whose_sum_over_a_group_passes_fp32(d, heads, pages):
+    rig = Rig(1, pages, heads, d, 16, seed=130)
+    rig.append([pages * 16 - 3])
+    q = np.sign(rig.rng.standard_normal((2, heads * 8, d))) * 3e38
+    q = np.where(np.arange(d) % 2 == 0, np.abs(q), q)    # eight of one sign in half of the channels
+    t = dev(q.astype(np.float32)).to(T().bfloat16)
+    q64 = f64(t)
+    for keep in (4, 40, 99):
+        got = guarded(rig, rig.batch([2]), t, 2, keep, 1, 1)
+        for i in range(2):
+            for h in range(heads):
+                assert got[i, h].tolist() == rig.ref.select(rig.table[0], h, q64[i, 8 * h:8 * h + 8], int(rig.len[0]) - 1 + i, keep, 1, 1), (keep, i, h)
+
+
+@pytest.mark.parametrize("pages", [100, 500, 9000])
+@pytest.mark.parametrize("what", [float("inf"), float("-inf"), float("nan")])
+def test_queries_that_are_no_numbers_still_give_lists_of_pages(pages, what):
+    rig = Rig(1, pages, 1, 64, 16, seed=131)
+    rig.append([pages * 16])
+    q, q64 = rig.draw(3, 2, 64)
+    bad = q.clone()
+    bad[1, 0, 5] = what
+    bad[2, :, :] = what
+    for keep in (4, 60):
+        got, want = guarded(rig, rig.batch([3]), bad, 3, keep, 2, 1), guarded(rig, rig.batch([3]), q, 3, keep, 2, 1)
+        assert np.array_equal(got[0], want[0])           # another row's list
+        for i in (1, 2):
+            own = got[i, 0]
+            assert (np.diff(own) > 0).all() and own[:2].tolist() == [0, 1] and own[-1] == pages - 1
