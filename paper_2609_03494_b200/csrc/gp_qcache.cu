@@ -489,7 +489,7 @@ constexpr int QS_BITS = 9;                   // of a key that a step of the desc
 constexpr int QS_CAP = 8192;                 // scores of a unit that the selection keeps in shared memory
 constexpr int QS_CLOSE = 256;                // pages close to the border that are ranked in shared memory
 constexpr double QS_UP = 0x1p860, QS_DOWN = 0x1p156;      // QS_UP * QS_DOWN = 2^1016
-constexpr float QS_ERR = 0x1p-16f * 448.f;   // error of a first score, of its scale times the sum of the weights' magnitudes (see there)
+constexpr float QS_ERR = 0x1p-14f * 448.f;   // error of a first score, of its scale times the sum of the weights' magnitudes (see there)
 
 // The integers that come out of the selection are those of scores in fp64; but only near the border does it take fp64 to know on which side a page lies.
 // So the tensor cores compute a first score with a bound on its error (a third of the time of fp64 throughout, which is bound by turning codes into
@@ -508,10 +508,11 @@ __device__ __forceinline__ double2 qs_weights(const unsigned short* q, int G, in
 // First scores of `chunk` pages for one (row, KV head): both kinds of sums are one product of the page's 2 d codes with the weights
 // [sum of min(q, 0), sum of max(q, 0)], whatever the group.  Pages are the rows of the products, codes fp16 (exact), the weights two columns: fp16, and
 // what that leaves times 2^11.  A lane reads 16 codes of a page at a time; the weights are read in the order in which four lanes then have them.
-// Error: the weights are off by 2^-22 of the largest, a product adds 16 exact terms to an fp32 sum, which it may cut off instead of rounding, so each
-// of the 2 d / 16 products is off by less than 17 * 2^-23 of what it adds up; together below 2^-17 of the sum of magnitudes, which is at most
-// 448 times the scale times the weights' sum of magnitudes: QS_ERR is twice that.  Both numbers are kept times 2^-30 (and the weights' power of two),
-// where fp32 holds them for every scale.
+// Error, with S the sum of magnitudes of all a page's terms (at most 448 times the scale times the weights' sum of magnitudes): a product adds 16 exact terms to
+// an fp32 sum and may cut each of the 17 off at 2^-23 of the largest, so each of the 2 d / 16 <= 16 products is off by less than 17 * 2^-23 of S (the sum so far may be
+// nearly all of S from the first product on), together by 2^-14.9 S.  The other column is off alike and counts 2^-11 of it; a weight in two parts is off by 2^-22 of
+// itself, the last addition and multiplication by 2^-23 each.  QS_ERR, 2^-14, is nearly twice the sum of these.  Both numbers are kept times 2^-30 (and the weights' power
+// of two), where fp32 holds them for every scale.
 template <int D>
 __global__ void __launch_bounds__(QS_THREADS)
 qc_score_kernel(const __grid_constant__ QcDev c, const unsigned short* __restrict__ q, long long q_stride, int Hq, int f16, int keep, int first, int recent,

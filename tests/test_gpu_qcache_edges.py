@@ -78,3 +78,29 @@ def test_queries_that_are_no_numbers_still_give_lists_of_pages(pages, what):
         for i in (1, 2):
             own = got[i, 0]
             assert (np.diff(own) > 0).all() and own[:2].tolist() == [0, 1] and own[-1] == pages - 1
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 1), (128, 1)])
+def test_scores_that_differ_in_their_last_bits_are_in_the_order_of_fp64(d, G):
+    """Nearly all of a score comes from channels of the first product that adds them up, at the largest code, and the order of the pages from what all the
+    products behind it add: codes of 2^-9 and 2^-8 against 448.  Bounds and scales are written here as an append of such keys would leave them."""
+    torch = T()
+    rig = Rig(1, 400, 1, d, 16, seed=132)
+    rig.len = np.array([400 * 16], np.int32)
+    rng = np.random.default_rng(5)
+    codes = rng.integers(0, 3, (402, 1, 2, d)).astype(np.uint8)      # 0, 2^-9, 2^-8
+    codes[:, :, 1, :16] = 0x7e                           # high: 448 in all pages
+    codes[:, :, 0, :16] = 0xfe                           # low: -448
+    codes[:, :, 0, 16:] = 0
+    rig.ref.bounds[:] = codes
+    rig.ref.exps[:] = 0
+    rig.bounds.view(torch.uint8).copy_(dev(codes))
+    rig.scales.fill_(1.0)
+    for n, small in enumerate((1.0, 2.0 ** -4, 2.0 ** -8)):
+        q = np.abs(rig.rng.standard_normal((1, G, d))) * small + small
+        q[:, :, :16] = np.sign(rig.rng.standard_normal((1, G, 16))) * (1 + np.arange(16) / 16)
+        t = dev(q.astype(np.float32)).to(torch.bfloat16)
+        q64 = f64(t)
+        for keep in (3, 57, 200, 390):
+            got = guarded(rig, rig.batch([1]), t, 1, keep, 0, 1)[0, 0].tolist()
+            assert got == rig.ref.select(rig.table[0], 0, q64[0], 6400, keep, 0, 1), (n, keep)
