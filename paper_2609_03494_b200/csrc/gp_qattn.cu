@@ -12,7 +12,6 @@ constexpr int QT_GRANULE = QT_WARPS * QT_TILES * 16;
 constexpr int QT_MIN_SHARE = 2;                // granules a thread block takes at least
 constexpr int QT_UNIT = 2;                     // what a unit costs beside its granules, in granules (its queries, the way to its first page, its end)
 constexpr float QT_LIFT = 8.f;                 // weights are carried times 2^8 ...
-constexpr float QT_NONE = -3.3e38f;            // a maximum of nothing
 constexpr float QT_SLACK = 7.f;                // ... while no logit is further above the maximum they refer to than this (base 2)
 
 constexpr int qt_resident(int nt, int d) { return nt * d <= 192 ? 3 : 2; }      // blocks of an SM that the registers allow
@@ -67,7 +66,7 @@ template <int D, int NT, int TERMS, bool LIST>
 __global__ void __launch_bounds__(QT_THREADS, qt_resident(NT, D))
 qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a, const __grid_constant__ CUtensorMap map) {
   constexpr int CH = D / 16;                            // 16-byte pieces of a token's codes
-  constexpr int ST = D + 2;
+  constexpr int ST = qt_part(D);
   constexpr int ROWS = 16 * D;                          // bytes of a tile's keys, or values
   constexpr int STAGE = QT_TILES * 2 * ROWS, STAGES = qt_stages(D);
   extern __shared__ uint8_t smem_raw[];
@@ -418,7 +417,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     if (__syncthreads_or(u.rows > 1 && bad)) {
       qt_plain<D>(c, a, u, reinterpret_cast<float*>(smem), part, 1);
     } else {
-      float* s_part = reinterpret_cast<float*>(smem);   // [warps][NT * 8][D + 2]
+      float* s_part = reinterpret_cast<float*>(smem);   // [warps][NT * 8] parts
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         const int col = n * 8 + (lane & 3) * 2, r = lane >> 2;
@@ -428,8 +427,8 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
 #pragma unroll
           for (int e = 0; e < 4; ++e) p0[(e & 1) * ST + j * 16 + 2 * r + (e >> 1)] = o[n][j][e];
         if (r == 0) {
-          p0[D] = m[n][0]; p0[D + 1] = l[n][0];
-          p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1];
+          p0[D] = m[n][0]; p0[D + 1] = l[n][0]; p0[D + 2] = 0.f;
+          p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1]; p0[ST + D + 2] = 0.f;
         }
       }
       __syncthreads();
@@ -480,13 +479,13 @@ QtPlan qt_plan(const QcDev& c, int G, int d, int n_list, bool list) {
   return p;
 }
 size_t qt_joins_bytes(const QtPlan& p) { return (size_t)p.blocks * 2 * sizeof(int4); }
-size_t qt_bytes(const QtPlan& p, int d) { return qt_joins_bytes(p) + (size_t)p.blocks * 2 * p.nt * 8 * (d + 2) * sizeof(float); }
+size_t qt_bytes(const QtPlan& p, int d) { return qt_joins_bytes(p) + (size_t)p.blocks * 2 * p.nt * 8 * qt_part(d) * sizeof(float); }
 
 template <int D, int NT, int TERMS, bool LIST>
 int qt_launch(const QcDev& c, const QtArgs& a, const CUtensorMap& map, const QtPlan& p, cudaStream_t s) {
   auto kern = qt_split_kernel<D, NT, TERMS, LIST>;
   size_t smem = QT_WARPS * qt_stages(D) * QT_TILES * 32 * D;
-  const size_t merge = (size_t)QT_WARPS * NT * 8 * (D + 2) * sizeof(float);
+  const size_t merge = (size_t)QT_WARPS * NT * 8 * qt_part(D) * sizeof(float);
   if (merge > smem) smem = merge;
   smem += 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return GP_ERR_CUDA;

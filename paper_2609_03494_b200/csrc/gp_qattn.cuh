@@ -11,6 +11,13 @@ constexpr int QT_THREADS = QT_WARPS * 32;
 // 68 / 69 / 70 / 71 (64 sequences: 95 / 139 / 246 / 256 and 202; one: 25 / 30 / 34 / 34 and 36).
 constexpr int qt_few(int d) { return d == 64 ? 64 : 24; }
 
+constexpr float QT_NONE = -3.3e38f;            // a maximum of nothing
+
+// A part of a column's result: D sums of weighted values, m, the sum of weights l, e (and a word that nobody reads).  With logits s to base 2, weights are 2^(s - m) and the
+// values' sums are held times 2^-e, so that no sum on the way passes what fp32 holds where the result does not: what is meant is 2^m l and 2^(m + e) o.
+// m and e are whole numbers in the kernels: what is rescaled loses no bits.
+__host__ __device__ constexpr int qt_part(int d) { return d + 4; }
+
 struct QtArgs {
   const unsigned short* q;
   long long q_stride;
@@ -18,7 +25,7 @@ struct QtArgs {
   const int* pages; int n_list;                // nullptr: all pages
   void* out; int out_type;
   int4* joins;                                 // [blocks][2] what qt_merge_kernel has to do
-  float* part;                                 // [blocks][2][columns][D + 2]
+  float* part;                                 // [blocks][2][columns][qt_part(D)]
   int few;                                     // qt_few
   unsigned by_g;                               // qt_row
   int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
@@ -55,29 +62,30 @@ __device__ __forceinline__ size_t qt_query(const QtArgs& a, const QtUnit& u, int
 // Four warps of a block (all of it, in the kernel that has no more) meet.
 __device__ __forceinline__ void qt_sync(int bar) { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); }
 
-// Joins the parts of a column: weights 2^(m - max).  p: [parts][stride] floats of a part's column: D values, m, sum.
+// Joins the parts of a column that a block's warps have.  s_part: [warps][cols_stride] parts.
 template <int D>
 __device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, float* part) {
-  constexpr int ST = D + 2;
+  constexpr int ST = qt_part(D);
   for (int i = threadIdx.x % QT_THREADS; i < u.cols * D; i += QT_THREADS) {
     const int col = i / D, e = i % D;
-    float M = -INFINITY;
+    auto p = [&](int w) { return s_part + (size_t)(w * cols_stride + col) * ST; };
+    float m = QT_NONE, top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) M = fmaxf(M, s_part[(size_t)(w * cols_stride + col) * ST + D]);
+    for (int w = 0; w < QT_WARPS; ++w) m = fmaxf(m, p(w)[D]);
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) top = fmaxf(top, p(w)[D] - m + p(w)[D + 2]);
     float o = 0.f, l = 0.f;
 #pragma unroll
     for (int w = 0; w < QT_WARPS; ++w) {
-      const float* p = s_part + (size_t)(w * cols_stride + col) * ST;
-      const float wt = M == -INFINITY ? 0.f : exp2f(p[D] - M);
-      o += wt * p[e];
-      l += wt * p[D + 1];
+      o += exp2f(p(w)[D] - m + p(w)[D + 2] - top) * p(w)[e];
+      l += exp2f(p(w)[D] - m) * p(w)[D + 1];
     }
     if (!part) {
-      qt_store(a.out, a.out_type, qt_query(a, u, col) * D + e, l != 0.f ? o / l : 0.f);      // (a NaN sum is not 0)
+      qt_store(a.out, a.out_type, qt_query(a, u, col) * D + e, l != 0.f ? o / l * exp2f(top) : 0.f);      // (a NaN sum is not 0)
     } else {
       float* dst = part + (size_t)col * ST;
       dst[e] = o;
-      if (e == 0) { dst[D] = M; dst[D + 1] = l; }
+      if (e == 0) *reinterpret_cast<float4*>(dst + D) = make_float4(m, l, top, 0.f);
     }
   }
 }
@@ -86,7 +94,7 @@ __device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const
 // NaN value that one row sees must not reach another through a weight of zero).
 template <int D>
 __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part, int bar) {
-  constexpr int PER = D / 32, ST = D + 2;
+  constexpr int PER = D / 32, ST = qt_part(D);
   const int warp = (threadIdx.x >> 5) % QT_WARPS, lane = threadIdx.x & 31;
   const float scale = 1.4426950408889634f * rsqrtf((float)D);
   for (int col = 0; col < u.cols; ++col) {
@@ -115,7 +123,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
     }
 #pragma unroll
     for (int e = 0; e < PER; ++e) smem[warp * ST + lane + 32 * e] = o[e];
-    if (lane == 0) { smem[warp * ST + D] = m; smem[warp * ST + D + 1] = l; }
+    if (lane == 0) { smem[warp * ST + D] = fmaxf(m, QT_NONE); smem[warp * ST + D + 1] = l; smem[warp * ST + D + 2] = 0.f; }
     qt_sync(bar);
     QtUnit one = u;
     one.cols = 1; one.row0 = row;
@@ -136,7 +144,7 @@ __device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u,
 template <int D, int COLS, int SLOTS>      // SLOTS: partial results a block has room for
 __global__ void __launch_bounds__(128)
 qt_merge_kernel(const __grid_constant__ QtArgs a) {
-  constexpr int ST = D + 2, PER = D / 64;               // pairs of elements a lane
+  constexpr int ST = qt_part(D), PER = D / 64;               // pairs of elements a lane
   const int lane = threadIdx.x & 31, at = blockIdx.x * 4 + (threadIdx.x >> 5), col = at % COLS, b = at / COLS;
   gp_pdl_wait();
   const int4 j = __ldcg(a.joins + b * 2);              // columns, the first part, the next block, the last block
@@ -144,23 +152,27 @@ qt_merge_kernel(const __grid_constant__ QtArgs a) {
   const int4 u = __ldcg(a.joins + b * 2 + 1);
   const int n_parts = j.w - j.z + 2;
   auto part = [&](int s) { return a.part + ((size_t)(s == 0 ? j.y : (j.z + s - 1) * SLOTS) * COLS + col) * ST; };
-  float M = -INFINITY, l = 0.f;
+  float m = QT_NONE, top = -INFINITY, l = 0.f;         // of the parts so far; o is held times 2^-top beside 2^-m
   float2 o[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) o[e] = make_float2(0.f, 0.f);
   for (int s0 = 0; s0 < n_parts; s0 += 32) {           // 32 parts at a time
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (s0 + lane < n_parts) ml = __ldcg(reinterpret_cast<const float2*>(part(s0 + lane) + D));
-    float mx = ml.x;
+    float4 x = make_float4(QT_NONE, 0.f, 0.f, 0.f);
+    if (s0 + lane < n_parts) x = __ldcg(reinterpret_cast<const float4*>(part(s0 + lane) + D));
+    float mx = x.x;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-    const float to = fmaxf(M, mx), corr = M == to ? 1.f : exp2f(M - to);
-    M = to;
-    const float w = to == -INFINITY ? 0.f : exp2f(ml.x - to);
-    float add = w * ml.y;
+    const float to = fmaxf(m, mx), at = x.x - to + x.z;
+    float tx = at;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) tx = fmaxf(tx, __shfl_xor_sync(0xffffffffu, tx, off));
+    const float was = top + (m - to), now = fmaxf(was, tx), corr = exp2f(was - now);
+    float add = exp2f(x.x - to) * x.y;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) add += __shfl_xor_sync(0xffffffffu, add, off);
-    l = l * corr + add;
+    l = l * exp2f(m - to) + add;
+    m = to; top = now;
+    const float w = exp2f(at - now);
 #pragma unroll
     for (int e = 0; e < PER; ++e) { o[e].x *= corr; o[e].y *= corr; }
     const int n = min(32, n_parts - s0);
@@ -170,18 +182,19 @@ qt_merge_kernel(const __grid_constant__ QtArgs a) {
       const float2* p = reinterpret_cast<const float2*>(part(s0 + s));
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        const float2 x = __ldcg(p + e * 32 + lane);
-        o[e].x += ws * x.x; o[e].y += ws * x.y;
+        const float2 y = __ldcg(p + e * 32 + lane);
+        o[e].x += ws * y.x; o[e].y += ws * y.y;
       }
     }
   }
   const int row = qt_row(a, col);
   const size_t rh = ((size_t)(u.x + row) * a.Hq + u.y * a.G + (col - row * a.G)) * D;
-  const float inv = l != 0.f ? 1.f / l : 0.f;          // (a NaN sum is not 0)
+  const float inv = l != 0.f ? 1.f / l : 0.f, scale = exp2f(top);      // (a NaN sum is not 0)
 #pragma unroll
   for (int e = 0; e < PER; ++e) {
     const size_t i = rh + (e * 32 + lane) * 2;
-    if (a.out_type == GP_TYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + i) = make_float2(o[e].x * inv, o[e].y * inv);
-    else *reinterpret_cast<uint32_t*>(static_cast<unsigned short*>(a.out) + i) = qc_pack(o[e].x * inv, o[e].y * inv, a.out_type == GP_TYPE_F16);
+    const float x = o[e].x * inv * scale, y = o[e].y * inv * scale;
+    if (a.out_type == GP_TYPE_F32) *reinterpret_cast<float2*>(static_cast<float*>(a.out) + i) = make_float2(x, y);
+    else *reinterpret_cast<uint32_t*>(static_cast<unsigned short*>(a.out) + i) = qc_pack(x, y, a.out_type == GP_TYPE_F16);
   }
 }

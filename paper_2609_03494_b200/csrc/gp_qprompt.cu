@@ -18,6 +18,8 @@ constexpr int QP_UNIT = 640;                   // what a unit costs beside its t
                                                // six sequences of 100 to 700 rows: 202 / 158 / 146 / 146 / 150)
 constexpr float QP_SLACK = 7.f;                // a row's maximum is brought up to date when something passes it by 2^7
 constexpr float QP_LIFT = 8.f;
+constexpr float QP_LAG = 30.f;                 // the maximum that the sum of weights refers to is brought up to date when a logit passes it by 2^30, or with the other
+constexpr float QP_FAR = 80.f;
 constexpr int QP_QBLOCK = QP_M * 128;          // bytes of 64 fp16 channels of the queries of a half
 constexpr int QP_BLOCK = QP_N * 128;           // ... of the tokens of a step
 
@@ -102,7 +104,7 @@ struct QpShared {
   int nan[8];                                  // by the number of the piece: that number, where a value is no number and rows see different tokens
   alignas(16) float ks[2 * QP_RING][QP_N / 16], ev[2 * QP_RING][QP_N / 16];      // per group of 16 tokens: scale of the keys (-1: no such page), exponent of that of the values
   long long x1, share, upto[QP_THREADS], warp[QP_THREADS / 32];
-  float plain[2][QT_WARPS * 130], qs[2][QP_M];
+  float plain[2][QT_WARPS * qt_part(128)], qs[2][QP_M];
 };
 // A bounded wait for a phase of a barrier.  (Without a time to suspend for, which brings a second look and a timer to each try: 627 -> 608 us.)
 __device__ __forceinline__ bool qp_try(uint32_t bar, uint32_t parity) {
@@ -235,10 +237,11 @@ struct QpWalk {
 // write them to shared memory as fp16, which holds them exactly and unscaled: K and V in the same image (a token's channels along a row, 64 a
 // swizzled 128 bytes), which the first product reads with the channels, the second with the tokens as inner dimension; four steps of them are there.
 // A warp more for each half issues its products.
-// Scales of pages cost nothing per element: 16 columns of S lie in one page, so the keys' scale joins the factor of the logits and the exponent of
-// the values' scale the constant that is added before the exponential: p' = 2^(s + ev - M), M the running maximum of s + ev.  O is then a plain
-// sum of p' times codes.  The sum of weights L is taken of p' 2^(E - ev) group by group, with E (an exponent of about the size of the largest ev so far)
-// keeping it in range (and no ev counted as less than E - 100); out = 2^E O / L.
+// Scales of pages cost nothing per element: 16 columns of S lie in one page, so the keys' scale joins the factor of the logits s and the exponent e of
+// the values' scale the constant that is added before the exponential: p' = 2^(s + e - M), M the running maximum of s + e of the tokens that the row sees.  O is then a plain
+// sum of p' times codes.  The sum of weights has a maximum of its own, m of s: L = sum of 2^(s - m), taken of p' group by group times 2^(M - m - e).  Both are whole
+// numbers, so that nothing is lost where they grow.  For that sum's sake no e counts as less than M - m - 80: a token of such a group has at most 2^-50 of the
+// largest p' then (its values count for nothing either way), and keeps a weight down to 2^-46 of the largest.  out = 2^(M - m) O / L.
 // Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 195 us, 845 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
 // d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2100 cycles for two
@@ -246,7 +249,7 @@ struct QpWalk {
 template <int D, int TERMS>
 __global__ void __launch_bounds__(QP_THREADS, 1)
 qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
-  constexpr int CH = D / 16, ST = D + 2;
+  constexpr int CH = D / 16, ST = qt_part(D);
   constexpr int QOPERAND = D / 64 * QP_QBLOCK, OPERAND = D / 64 * QP_BLOCK;      // bytes of a half's Q, of a step's K or V in shared memory
   // tensor memory: two S (and P over them) and O of each half; the second terms of the weights over the S columns that P leaves free
   constexpr uint32_t T_S = 0, T_O = 256;
@@ -479,8 +482,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       }
       __syncwarp();
       if (lane == 0 && p.n_steps > 0) qp_arrive(&sh.q_full[half]);
-      float M = -INFINITY, L = 0.f;                     // M: less the lift
-      float E = 0.f;                                    // set at the first step
+      float M = -INFINITY, m = -INFINITY, L = 0.f;      // M: less the lift
       for (int j = 0; j < p.n_steps; ++j) {
         const int s = n + j;
         const int slot = s & (2 * QP_RING - 1);
@@ -493,21 +495,9 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           int masked = t0 + QP_N > least || fminf(fminf(kq.x, kq.y), fminf(kq.z, kq.w)) < 0.f;      // some row does not see all of the step
           const float ks[4] = {kq.x, kq.y, kq.z, kq.w};
           float ev[4] = {eq.x, eq.y, eq.z, eq.w};
-          float top = -1000.f, f[4];
+          float f[4];
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            f[g] = fmaxf(ks[g] * qs, 1.2e-38f);
-            if (ks[g] >= 0.f) top = fmaxf(top, ev[g]);
-          }
-          // E, and the exponents as far as they matter beside it: values 2^100 below E's (a page of zeros has the smallest exponent there is) may count as
-          // 2^-100 times E's, their weights count alike
-          float dE = 0.f;
-          if (top > -1000.f) {
-            if (j == 0) E = top;
-            else if (top > E + 40.f) { dE = top - E; E = top; }
-          }
-#pragma unroll
-          for (int g = 0; g < 4; ++g) ev[g] = fmaxf(ev[g], E - 100.f);
+          for (int g = 0; g < 4; ++g) f[g] = fmaxf(ks[g] * qs, 1.2e-38f);
           float x0[32], x1[32];
 #pragma unroll 1
           for (;;) {
@@ -529,7 +519,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             masked = 0;
             asm volatile("" : "+r"(masked));            // (or the compiler makes two of it)
           }
-          float mx = -INFINITY;                         // the largest s + ev of the step
+          float mx = -INFINITY, ms = -INFINITY;         // the step's largest s + e and s
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const float* x = (g & 2 ? x1 : x0) + (g & 1) * 16;
@@ -537,18 +527,17 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             m0 = qp_max3(m0, x[6], x[7]); m1 = qp_max3(m1, x[8], x[9]);
             m0 = qp_max3(m0, x[10], x[11]); m1 = qp_max3(m1, x[12], x[13]);
             m0 = qp_max3(m0, x[14], x[15]);
-            mx = fmaxf(mx, fmaf(fmaxf(m0, m1), f[g], ev[g]));
+            const float t = fmaxf(m0, m1) * f[g];
+            ms = fmaxf(ms, t); mx = fmaxf(mx, t + ev[g]);
           }
-          const bool over = mx > M + (QP_LIFT + QP_SLACK);
-          if (__any_sync(0xffffffffu, over || dE != 0.f)) {
+          const bool over = mx > M + (QP_LIFT + QP_SLACK) || ms > m + QP_LAG;
+          if (__any_sync(0xffffffffu, over)) {
             float corr = 1.f;
             if (over) {
-              const float to = mx - QP_LIFT, by = M - to;      // (-infinity at first)
-              corr = qt_exp2(by);
-              L = L > 0.f ? L * qt_exp2(fminf(dE + by, 100.f)) : L * corr;
-              M = to;
-            } else if (dE != 0.f) {
-              L *= qt_exp2(fminf(dE, 100.f));
+              const float to = fmaxf(M, ceilf(mx) - QP_LIFT), top = fmaxf(m, ceilf(ms));      // (minus infinity at first)
+              corr = qt_exp2(M - to);
+              L *= qt_exp2(m - top);
+              M = to; m = top;
             }
             if (j > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
               qp_wait(sh, &sh.o_full[half][(s - 1) & (QP_RING - 1)], ((s - 1) / QP_RING) & 1);      // all of O is there
@@ -564,7 +553,9 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
               }
             }
           }
-          const float zero = M == -INFINITY ? 0.f : M;
+          const float zero = M == -INFINITY ? 0.f : M, apart = M == -INFINITY ? 0.f : M - m;
+#pragma unroll
+          for (int g = 0; g < 4; ++g) ev[g] = fmaxf(ev[g], apart - QP_FAR);
           qp_turn(turn + half);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {                 // weights of 16 columns to tensor memory
@@ -588,7 +579,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             }
             float s0, s1;
             qp_unpack2(acc, s0, s1);
-            L = fmaf(s0 + s1, qt_exp2(E - ev[g]), L);
+            L = fmaf(s0 + s1, qt_exp2(apart - ev[g]), L);
             qp_st8(t_x + g * 8, hi);
             if (TERMS == 2) qp_st8(t_x + 32 + g * 8, lo);
           }
@@ -608,15 +599,13 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         qp_fence_after();
       }
       if (!used) continue;
-      // out = 2^E O / L; a part of a result: 2^E O, M - E, L
-      const float scale = exp2f(E), inv = L != 0.f ? scale / L : 0.f;      // (a NaN sum is not 0)
       float* parts = p.whole ? nullptr : a.part + (size_t)(blockIdx.x * 2 + (p.begins ? 0 : 1)) * QP_COLS * ST + (size_t)half * RT * a.G * ST;
       // by way of the memory of the warp's own 32 queries (no product reads them any more), so that lanes store what lies together
       const uint32_t stage = q_smem + half * QOPERAND + (warp & 3) * (32 * 128);
       auto place = [&](int col, int pc) { return stage + (pc >> 3) * QP_QBLOCK + col * 128 + (((pc & 7) ^ (col & 7)) << 4); };
       constexpr int PIECES = D / 8;                     // of 16 bytes, of a column there
       const bool wide = parts || a.out_type == GP_TYPE_F32;      // two rounds of half of the channels in 32 bits, else one of all in 16
-      const float by = parts ? scale : inv;
+      const float apart = M == -INFINITY ? 0.f : M - m, inv = parts ? 1.f : L != 0.f ? 1.f / L : 0.f, scale = parts ? 1.f : exp2f(apart);      // (a NaN sum is not 0)
 #pragma unroll 1
       for (int round = 0; round < (wide ? 2 : 1); ++round) {
         const int chans = wide ? D / 2 : D;
@@ -632,7 +621,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             for (int e = 0; e < 16; ++e) o[e] = 0.f;
           }
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] *= by;
+          for (int e = 0; e < 16; ++e) o[e] = o[e] * inv * scale;
           if (wide) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -673,7 +662,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         }
         __syncwarp();
       }
-      if (parts && real) { parts[(size_t)t128 * ST + D] = M == -INFINITY ? M : M - E; parts[(size_t)t128 * ST + D + 1] = L; }
+      if (parts && real) *reinterpret_cast<float4*>(parts + (size_t)t128 * ST + D) = make_float4(fmaxf(m, QT_NONE), L, apart, 0.f);
       if (p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece)      // some row may have met another's NaN: all of the half in plain arithmetic
         qt_plain<D>(c, a, u, sh.plain[half], parts, 1 + half);
     }
@@ -709,7 +698,7 @@ QpPlan qp_plan(const QcDev& c, int G) {
   p.blocks = (int)(blocks < 148 ? blocks : 148);                                 // a block has an SM's tensor memory
   return p;
 }
-size_t qp_bytes(const QpPlan& p, int d) { return (size_t)p.blocks * 2 * (sizeof(int4) + (size_t)QP_COLS * (d + 2) * sizeof(float)); }
+size_t qp_bytes(const QpPlan& p, int d) { return (size_t)p.blocks * 2 * (sizeof(int4) + (size_t)QP_COLS * qt_part(d) * sizeof(float)); }
 int qp_launch(const QcDev& c, QtArgs a, const QpPlan& p, int d, void* work, cudaStream_t s) {
   a.joins = static_cast<int4*>(work);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(work) + (size_t)p.blocks * 2 * sizeof(int4));

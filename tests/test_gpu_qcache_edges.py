@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_qcache import Rig, T, dev, f64
+from tests.test_gpu_qcache import BF16, EPS, F32, Rig, T, dev, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,96 @@ def test_scores_that_differ_in_their_last_bits_are_in_the_order_of_fp64(d, G):
         for keep in (3, 57, 200, 390):
             got = guarded(rig, rig.batch([1]), t, 1, keep, 0, 1)[0, 0].tolist()
             assert got == rig.ref.select(rig.table[0], 0, q64[0], 6400, keep, 0, 1), (n, keep)
+
+
+# ------------------------------------------------------------------------------------------------ scales of values far apart
+def along(rig, logits):
+    """Keys whose logit (base 2) for a query of ones in channel 0 is about what is given; queries like that."""
+    k = np.zeros((len(logits), rig.heads, rig.d), np.float32)
+    k[:, :, 0] = (np.asarray(logits, np.float64) * np.log(2) * np.sqrt(rig.d))[:, None]
+    t = dev(k).to(T().bfloat16)
+    return t, f64(t)
+
+
+def values(rig, n, size):
+    """About `size`, of one sign: 1 + 0.1 N(0, 1)."""
+    t = dev(((1 + 0.1 * rig.rng.standard_normal((n, rig.heads, rig.d))) * size).astype(np.float32)).to(T().bfloat16)
+    return t, f64(t)
+
+
+def ones(rig, rows, G):
+    q = np.zeros((rows, rig.heads * G, rig.d), np.float32)
+    q[:, :, 0] = 1 + 0.01 * rig.rng.random((rows, rig.heads * G))
+    t = dev(q).to(T().bfloat16)
+    return t, f64(t)
+
+
+def check_sharp(rig, rows, q64, out, out_dtype, pages=None):
+    """Like check_attention, against a bound that a large value without weight does not widen.  With t_j = 448 * 2^e_j, e_j the exponent of the scale of token
+    j's values, and w_j its weight:
+      weights carry a relative error of 2 (d 2^-22 A + 2^-18), and 2^-12 more for 16-bit results: that of the weighted sum of magnitudes;
+      fp16 holds a weight down to 2^-25 where the largest is 2^7 at least, so a token may lose 2^-32 of the largest weight (few rows), or of the largest
+      product of weight and scale (many rows, twice that as a scale's largest value is only known to a factor of two): counted as 2^-31 of both;
+      sums are kept relative to the largest scale of the sequence, in numbers down to 2^-149."""
+    got, at, G = f64(out), 0, q64.shape[1] // rig.heads
+    for s, r in enumerate(rows):
+        for i in range(r):
+            n = int(rig.len[s]) - r + i + 1
+            for h in range(rig.heads):
+                k, v, ok = rig.ref.rows(rig.table[s], h, n)
+                top = np.ldexp(448.0, rig.ref.exps[rig.table[s][np.arange(n) // rig.page], h, 1])
+                most = np.ldexp(448.0, int(rig.ref.exps[rig.table[s][:-(-int(rig.len[s]) // rig.page)], h, 1].max()))
+                if pages is not None:
+                    ok &= np.isin(np.arange(n) // rig.page, pages[at, h])
+                k, v, top = k[ok], v[ok], top[ok]
+                for g in range(G):
+                    x = k @ q64[at, h * G + g] / np.sqrt(rig.d)
+                    w = np.exp(x - x.max())
+                    w /= w.sum()
+                    A = float((np.abs(k) @ np.abs(q64[at, h * G + g])).max()) / np.sqrt(rig.d)
+                    ref, size = w @ v, w @ np.abs(v)
+                    rel = 2 * (rig.d * 2.0 ** -22 * A + 2.0 ** -18) + (0 if out_dtype == F32 else 2.0 ** -12)
+                    tol = rel * size + np.minimum(w, 2.0 ** -31 * w.max()) @ top + len(w) * 2.0 ** -31 * (w * top).max() + EPS[out_dtype] / 2 * np.abs(ref) + most * 2.0 ** -146
+                    err = np.abs(got[at, h * G + g] - ref)
+                    assert (err <= tol).all(), (s, i, h, g, float(err.max()), float(tol.min()), float(np.abs(ref).max()))
+            at += 1
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("rows", [1, 5, 40, 150])
+def test_the_sum_of_weights_holds_when_far_smaller_values_come_first(d, G, rows):
+    """Zeros first (the smallest scale there is), then values whose weights are 2^-110 of theirs, then values whose weights are equal to theirs: the zeros count for half."""
+    rig = Rig(1, 30, 1, d, 16, seed=120)
+    zero = dev(np.zeros((64, 1, d), np.float32)).to(T().bfloat16)
+    rig.append([64], kv=(along(rig, [0] * 64), (zero, f64(zero))))
+    rig.append([64], kv=(along(rig, [-110] * 64), values(rig, 64, 1.0)))
+    rig.append([64], kv=(along(rig, [0] * 64), values(rig, 64, 1.0)))
+    rig.append([rows], kv=(along(rig, [-110] * rows), values(rig, rows, 1.0)))
+    q, q64 = ones(rig, rows, G)
+    for out in (F32, BF16):
+        check_sharp(rig, [rows], q64, rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)), out)
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("rows", [5, 40, 150])
+def test_far_larger_values_that_a_row_does_not_see_change_nothing_for_it(d, G, rows):
+    rig = Rig(1, 40, 2, d, 16, seed=121)
+    rig.append([301], kv=(rig.draw(301, 2, d), values(rig, 301, 1.0)))
+    rig.append([rows - 2], kv=(rig.draw(rows - 2, 2, d), values(rig, rows - 2, 1e-3)))
+    rig.append([2], kv=(rig.draw(2, 2, d), values(rig, 2, 1e36)))
+    q, q64 = rig.draw(rows, 2 * G, d)
+    for out in (F32, BF16):
+        check_sharp(rig, [rows], q64, rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)), out)
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("rows", [1, 5, 40, 150])
+@pytest.mark.parametrize("logit", [-300, -140])
+def test_far_larger_values_without_weight_leave_the_others_what_they_are(d, G, rows, logit):
+    rig = Rig(1, 40, 1, d, 16, seed=122)
+    rig.append([48], kv=(along(rig, [logit] * 48), values(rig, 48, 2.0 ** 110)))
+    rig.append([200], kv=(along(rig, [0] * 200), values(rig, 200, 1.0)))
+    rig.append([rows], kv=(along(rig, [0] * rows), values(rig, rows, 2.0 ** -10)))
+    q, q64 = ones(rig, rows, G)
+    for out in (F32, BF16):
+        check_sharp(rig, [rows], q64, rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)), out)
