@@ -185,6 +185,14 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         w.ks = s.x; w.vs = s.y;
       }
     };
+    // scales of values from here on times 2^-e
+    uint32_t top = (uint32_t)(QC_E_MIN + 127) << 23;    // 2^e
+    auto scaled = [&](Where& w) {                       // of 32 more tiles; what O is to be multiplied with
+      const uint32_t was = top;
+      top = max(top, __reduce_max_sync(0xffffffffu, __float_as_uint(w.vs)));
+      w.vs *= 1.f / __uint_as_float(top);
+      return __uint_as_float(was) / __uint_as_float(top);
+    };
     Where cur = look(lane), nxt;
     nxt.id = -1; nxt.tok = nxt.left = 0; nxt.ks = nxt.vs = 0.f;
     if (n_stages * QT_TILES > 32 * QT_WARPS) nxt = look(32 + lane);
@@ -260,10 +268,18 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     const int mi = lane >> 3, mr = lane & 7;            // ldmatrix: matrix and row this lane addresses
     const int lt = mr + (mi & 1) * 8, lsw = D == 128 ? lt & 7 : (lt >> 1) & 3;
     int batch = 0;
+    scaled(cur);                                        // (here: copies and queries are asked for before the scales have come)
     for (int i = 0; i * QT_WARPS + warp < n_stages; ++i) {
       if ((i * QT_TILES >> 5) != batch) {               // 32 tiles on: `nxt` holds these, ask for the ones behind
         ++batch;
         cur = nxt;
+        const float by = scaled(cur);
+        if (by != 1.f) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) { o[n][j][0] *= by; o[n][j][1] *= by; o[n][j][2] *= by; o[n][j][3] *= by; }
+        }
         nxt = look((batch + 1) * 32 + lane);
         look_scales(nxt);
       }
@@ -350,7 +366,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
           float corr[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float mn = fmaxf(m[n][e], mx[e] - QT_LIFT);
+            const float mn = fmaxf(m[n][e], ceilf(mx[e]) - QT_LIFT);
             corr[e] = m[n][e] == mn ? 1.f : qt_exp2(m[n][e] - mn);
             m[n][e] = mn;
           }
@@ -427,8 +443,9 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
 #pragma unroll
           for (int e = 0; e < 4; ++e) p0[(e & 1) * ST + j * 16 + 2 * r + (e >> 1)] = o[n][j][e];
         if (r == 0) {
-          p0[D] = m[n][0]; p0[D + 1] = l[n][0]; p0[D + 2] = 0.f;
-          p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1]; p0[ST + D + 2] = 0.f;
+          p0[D] = m[n][0]; p0[D + 1] = l[n][0];
+          p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1];
+          p0[D + 2] = p0[ST + D + 2] = (float)((int)(top >> 23) - 127);
         }
       }
       __syncthreads();

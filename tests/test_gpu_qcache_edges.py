@@ -197,3 +197,35 @@ def test_far_larger_values_without_weight_leave_the_others_what_they_are(d, G, r
     q, q64 = ones(rig, rows, G)
     for out in (F32, BF16):
         check_sharp(rig, [rows], q64, rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)), out)
+
+
+# ------------------------------------------------------------------------------------------------ values at the upper end of the range
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("rows", [1, 5, 40, 150])
+@pytest.mark.parametrize("n", [1, 300, 9000])
+@pytest.mark.parametrize("size", [2.0 ** 112, 2.0 ** 126, 2.0 ** -118])
+def test_values_at_the_ends_of_the_range(d, G, rows, n, size):
+    """Every held value is at most 448 * 2^119, and so is a weighted mean of them: sums on the way are not to pass what fp32 holds, in whole units and in
+    those that blocks share (one KV head of 9000 tokens)."""
+    rig = Rig(1, 600, 1, d, 16, seed=123)
+    rig.append([n], kv=(rig.draw(n, 1, d), values(rig, n, size)))
+    rig.append([rows], kv=(rig.draw(rows, 1, d), values(rig, rows, size)))
+    q, q64 = rig.draw(rows, G, d)
+    some = sorted({0, rows // 2, rows - 1})
+    for out in (F32, BF16):
+        got = rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out))
+        for i in some:
+            one = Rig.__new__(Rig)
+            one.__dict__.update(rig.__dict__)
+            one.len = rig.len - (rows - 1 - i)
+            check_sharp(one, [1], q64[i:i + 1], got[i:i + 1], out)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 112, 2.0 ** 126])
+def test_values_at_the_upper_end_of_the_range_through_a_list(size):
+    rig = Rig(1, 600, 1, 128, 16, seed=124)
+    rig.append([9000], kv=(rig.draw(9000, 1, 128), values(rig, 9000, size)))
+    q, q64 = rig.draw(1, 4, 128)
+    pages = rig.gpu.select(rig.batch([1]), q, 500, 1, 1)
+    for out in (F32, BF16):
+        check_sharp(rig, [1], q64, rig.gpu.attention(rig.batch([1]), q, out_dtype=getattr(T(), out), pages=pages), out, pages.cpu().numpy())
