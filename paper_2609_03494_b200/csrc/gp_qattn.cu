@@ -27,6 +27,35 @@ __device__ __forceinline__ void qt_tma_rows(uint32_t dst_smem, const CUtensorMap
                "r"(0), "r"(row), "r"(page), "r"(bar)
                : "memory");
 }
+// Joins the parts of a column that a block's warps have.  s_part: [warps][cols_stride] parts; nan (or null): per channel the least row that sees a value that is no number.
+template <int D>
+__device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, const int* nan, float* part) {
+  constexpr int ST = qt_part(D);
+  for (int i = threadIdx.x; i < u.cols * D; i += QT_THREADS) {
+    const int col = i / D, e = i % D;
+    auto p = [&](int w) { return s_part + (size_t)(w * cols_stride + col) * ST; };
+    float m = QT_NONE, top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) m = fmaxf(m, p(w)[D]);
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) top = fmaxf(top, p(w)[D] - m + p(w)[D + 2]);
+    float o = 0.f, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < QT_WARPS; ++w) {
+      o += exp2f(p(w)[D] - m + p(w)[D + 2] - top) * p(w)[e];
+      l += exp2f(p(w)[D] - m) * p(w)[D + 1];
+    }
+    if (nan && nan[e] <= qt_row(a, col)) o = __int_as_float(0x7fffffff);
+    if (!part) {
+      qt_store(a.out, a.out_type, qt_query(a, u, col) * D + e, l != 0.f ? o / l * exp2f(top) : 0.f);      // (a NaN sum is not 0)
+    } else {
+      float* dst = part + (size_t)col * ST;
+      dst[e] = o;
+      if (e == 0) *reinterpret_cast<float4*>(dst + D) = make_float4(m, l, top, 0.f);
+    }
+  }
+}
+
 // The work of a call is one line of granules (the tokens that a block's warps take at a time): sequence by sequence, KV head by KV head, tile of
 // rows by tile of rows.  Every thread block takes the same stretch of it, whatever the lengths: none waits for a long sequence at the end, and
 // only the first and the last unit of a stretch can be shared with other blocks, so two partial results per block are all there is.
@@ -58,6 +87,8 @@ __device__ __forceinline__ long long qt_head_granules(const QcDev& c, const QtAr
 // Keys: ldmatrix gives a lane four consecutive codes of a token, which are its elements of both halves of a k step when the queries are
 // read in the same order.  Values: ldmatrix.trans moves pairs of codes, i.e. two channels of two tokens in a register; a byte permutation
 // puts them in pairs of tokens, and the two channels go to rows r and r + 8 of the product.
+// Values that are no numbers: a weight of 0 would carry them to rows that do not see them.  Where the rows of a tile see different tokens, the codes of tokens that
+// not all of them see are looked at in shared memory; a NaN counts as 0 there, and at the end the least row that sees one is found per channel.
 // A warp brings its own tiles in, two at a time by TMA, into its own stages: nothing in the loop waits for another warp.
 // What bounds it: memory where sequences are long (three of 60 001 to 131 071 tokens, 8 KV heads, groups of 8, d = 128: 116 us, 6.2 TB/s); where they
 // are short, the start and end of a block's units (64 of 60 to 4000 tokens, groups of 4: 51 us, 5.2 TB/s); with many columns, instructions (five rows of 48
@@ -72,9 +103,13 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
   extern __shared__ uint8_t smem_raw[];
   __shared__ long long s_upto[QT_THREADS], s_warp[QT_WARPS];
   __shared__ __align__(8) uint64_t s_bar[QT_WARPS][STAGES];
+  __shared__ int s_nan[D], s_found;
+  __shared__ uint32_t s_top[QT_WARPS];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);      // (the swizzle goes by the address)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid < QT_WARPS * STAGES) mbar_init(&s_bar[0][0] + tid, 1);
+  if (tid < D) s_nan[tid] = 0x7fffffff;
+  if (tid == 0) s_found = 0;
   fence_mbar_init();
   if (LIST) gp_pdl_wait();                              // the list may come from the kernel before
   gp_pdl_launch_dependents();
@@ -185,12 +220,13 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         w.ks = s.x; w.vs = s.y;
       }
     };
-    // scales of values from here on times 2^-e
-    uint32_t top = (uint32_t)(QC_E_MIN + 127) << 23;    // 2^e
-    auto scaled = [&](Where& w) {                       // of 32 more tiles; what O is to be multiplied with
-      const uint32_t was = top;
-      top = max(top, __reduce_max_sync(0xffffffffu, __float_as_uint(w.vs)));
+    // scales of values of 32 more tiles times 2^-e, with `was` the 2^e so far; what O is to be multiplied with
+    auto scaled = [&](Where& w, uint32_t was) {
+      const uint32_t top = max(was, __reduce_max_sync(0xffffffffu, __float_as_uint(w.vs)));
       w.vs *= 1.f / __uint_as_float(top);
+      __syncwarp();
+      if (lane == 0) s_top[warp] = top;
+      __syncwarp();
       return __uint_as_float(was) / __uint_as_float(top);
     };
     Where cur = look(lane), nxt;
@@ -268,12 +304,12 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     const int mi = lane >> 3, mr = lane & 7;            // ldmatrix: matrix and row this lane addresses
     const int lt = mr + (mi & 1) * 8, lsw = D == 128 ? lt & 7 : (lt >> 1) & 3;
     int batch = 0;
-    scaled(cur);                                        // (here: copies and queries are asked for before the scales have come)
+    scaled(cur, (uint32_t)(QC_E_MIN + 127) << 23);      // (here: copies and queries are asked for before the scales have come)
     for (int i = 0; i * QT_WARPS + warp < n_stages; ++i) {
       if ((i * QT_TILES >> 5) != batch) {               // 32 tiles on: `nxt` holds these, ask for the ones behind
         ++batch;
         cur = nxt;
-        const float by = scaled(cur);
+        const float by = scaled(cur, s_top[warp]);
         if (by != 1.f) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -304,6 +340,32 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         most = max(most, left[k]); end = max(end, tok[k]);
       }
       if (most <= 0) { __syncwarp(); continue; }
+      const bool ragged = end + 16 > vis0;              // some column does not see all of the stage
+      if (ragged) {
+#pragma unroll
+        for (int k = 0; k < QT_TILES; ++k) {
+          // rows behind the sequence, and tiles that are not there: whatever an earlier owner or tile left, NaN too
+          for (int r = max(left[k], 0) * (D / 16) + lane; r < D; r += 32)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (k * 2 + 1) * ROWS + r * 16), "r"(0) : "memory");
+          // rows that some column does not see
+          for (int r = max(vis0 - tok[k], 0) * (D / 16) + lane; r < min(left[k], 16) * (D / 16); r += 32) {
+            const uint32_t at = stage + (k * 2 + 1) * ROWS + r * 16;
+            uint32_t w[4], any = 0;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t bad = __vcmpeq4(w[e] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              w[e] &= ~bad; any |= bad;
+            }
+            if (any) {
+              s_found = 1;
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+            }
+          }
+        }
+        fence_proxy_async();                            // the next copy into the stage comes behind these stores
+        __syncwarp();
+      }
       float s[QT_TILES][NT][4];
       auto factor = [&](int k, int n, int e) { return fmaxf(kf[k] * qs[n][e], 1.2e-38f); };      // (above 0: a masked logit stays what it is)
       // (d = 64: no branch on what a tile holds lies between the tiles of a stage, so that one's instructions fill the other's waits, 73 -> 70 us for five
@@ -327,7 +389,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
           }
         }
       }
-      if (end + 16 > vis0) {                            // some column does not see all of the stage
+      if (ragged) {
 #pragma unroll
         for (int k = 0; k < QT_TILES; ++k) {
 #pragma unroll
@@ -335,12 +397,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (tok[k] + (lane >> 2) + (e >> 1) * 8 >= qt_visible(c, a, u, n * 8 + (lane & 3) * 2 + (e & 1))) s[k][n][e] = -INFINITY;
-          // rows behind the sequence, and tiles that are not there: whatever an earlier owner or tile left, NaN too
-          for (int r = max(left[k], 0) * (D / 16) + lane; r < D; r += 32)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(stage + (k * 2 + 1) * ROWS + r * 16), "r"(0) : "memory");
         }
-        fence_proxy_async();                            // the next copy into the stage comes behind these stores
-        __syncwarp();
       }
       bool over = false;
 #pragma unroll
@@ -416,7 +473,6 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
       }
       __syncwarp();                                     // the stage has been read: it may be fetched into
     }
-    bool bad = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -424,35 +480,41 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         l[n][0] += __shfl_xor_sync(0xffffffffu, l[n][0], off);
         l[n][1] += __shfl_xor_sync(0xffffffffu, l[n][1], off);
       }
-      if (!LIST)
-#pragma unroll
-        for (int j = 0; j < CH; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bad |= !(fabsf(o[n][j][e]) < INFINITY) && n * 8 + (lane & 3) * 2 + (e & 1) < u.cols;
     }
-    if (__syncthreads_or(u.rows > 1 && bad)) {
-      qt_plain<D>(c, a, u, reinterpret_cast<float*>(smem), part, 1);
-    } else {
-      float* s_part = reinterpret_cast<float*>(smem);   // [warps][NT * 8] parts
+    __syncthreads();
+    const bool nans = s_found != 0;
+    float* s_part = reinterpret_cast<float*>(smem);     // [warps][NT * 8] parts
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const int col = n * 8 + (lane & 3) * 2, r = lane >> 2;
-        float* p0 = s_part + (size_t)(warp * NT * 8 + col) * ST;
+    for (int n = 0; n < NT; ++n) {
+      const int col = n * 8 + (lane & 3) * 2, r = lane >> 2;
+      float* p0 = s_part + (size_t)(warp * NT * 8 + col) * ST;
 #pragma unroll
-        for (int j = 0; j < CH; ++j)
+      for (int j = 0; j < CH; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p0[(e & 1) * ST + j * 16 + 2 * r + (e >> 1)] = o[n][j][e];
-        if (r == 0) {
-          p0[D] = m[n][0]; p0[D + 1] = l[n][0];
-          p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1];
-          p0[D + 2] = p0[ST + D + 2] = (float)((int)(top >> 23) - 127);
-        }
+        for (int e = 0; e < 4; ++e) p0[(e & 1) * ST + j * 16 + 2 * r + (e >> 1)] = o[n][j][e];
+      if (r == 0) {
+        p0[D] = m[n][0]; p0[D + 1] = l[n][0];
+        p0[ST + D] = m[n][1]; p0[ST + D + 1] = l[n][1];
+        p0[D + 2] = p0[ST + D + 2] = (float)((int)(s_top[warp] >> 23) - 127);
       }
-      __syncthreads();
-      qt_write<D>(a, u, s_part, NT * 8, part);
     }
+    if (nans)                                           // once more, from the cache: which channels, which rows
+      for (int i = tid; i < (u.t1 - max(u.t0, vis0)) * (D / 4); i += QT_THREADS) {
+        const int t = max(u.t0, vis0) + i / (D / 4), id = qc_page(c, seq, t >> c.page_log);
+        if (id < 0) continue;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(c.codes + (((size_t)id * c.Hkv + u.h) * 2 * c.page + c.page + (t & (c.page - 1))) * D + i % (D / 4) * 4);
+        for (int e = 0; e < 4; ++e)
+          if ((w >> (8 * e) & 0x7f) == 0x7f) atomicMin(&s_nan[i % (D / 4) * 4 + e], t + 1 - vis0);
+      }
+    __syncthreads();
+    qt_write<D>(a, u, s_part, NT * 8, nans ? s_nan : nullptr, part);
     fence_proxy_async();
     __syncthreads();                                    // the memory is the ring's again
+    if (nans) {
+      if (tid < D) s_nan[tid] = 0x7fffffff;
+      if (tid == 0) s_found = 0;
+      __syncthreads();
+    }
   }
   if (gave_up && c.status) atomicOr(c.status, GP_E_SPIN);
 }

@@ -1,4 +1,4 @@
-// What the two attention kernels of the 8-bit cache share: arguments, units of work, how warps' and blocks' parts of a result are joined.
+// What the two attention kernels of the 8-bit cache share: arguments, units of work, how blocks' parts of a result are joined.
 #pragma once
 #include "gp_qcache.cuh"
 
@@ -59,86 +59,6 @@ __device__ __forceinline__ size_t qt_query(const QtArgs& a, const QtUnit& u, int
   const int r = qt_row(a, col);
   return (size_t)(u.row0 + r) * a.Hq + u.h * a.G + (col - r * a.G);
 }
-// Four warps of a block (all of it, in the kernel that has no more) meet.
-__device__ __forceinline__ void qt_sync(int bar) { asm volatile("bar.sync %0, 128;" ::"r"(bar) : "memory"); }
-
-// Joins the parts of a column that a block's warps have.  s_part: [warps][cols_stride] parts.
-template <int D>
-__device__ __forceinline__ void qt_write(const QtArgs& a, const QtUnit& u, const float* s_part, int cols_stride, float* part) {
-  constexpr int ST = qt_part(D);
-  for (int i = threadIdx.x % QT_THREADS; i < u.cols * D; i += QT_THREADS) {
-    const int col = i / D, e = i % D;
-    auto p = [&](int w) { return s_part + (size_t)(w * cols_stride + col) * ST; };
-    float m = QT_NONE, top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) m = fmaxf(m, p(w)[D]);
-#pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) top = fmaxf(top, p(w)[D] - m + p(w)[D + 2]);
-    float o = 0.f, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < QT_WARPS; ++w) {
-      o += exp2f(p(w)[D] - m + p(w)[D + 2] - top) * p(w)[e];
-      l += exp2f(p(w)[D] - m) * p(w)[D + 1];
-    }
-    if (!part) {
-      qt_store(a.out, a.out_type, qt_query(a, u, col) * D + e, l != 0.f ? o / l * exp2f(top) : 0.f);      // (a NaN sum is not 0)
-    } else {
-      float* dst = part + (size_t)col * ST;
-      dst[e] = o;
-      if (e == 0) *reinterpret_cast<float4*>(dst + D) = make_float4(m, l, top, 0.f);
-    }
-  }
-}
-
-// The unit in plain arithmetic, a warp a token and column after column: for a result that is not finite where rows see different tokens (a
-// NaN value that one row sees must not reach another through a weight of zero).
-template <int D>
-__device__ __noinline__ void qt_plain(const QcDev& c, const QtArgs& a, QtUnit u, float* smem, float* part, int bar) {
-  constexpr int PER = D / 32, ST = qt_part(D);
-  const int warp = (threadIdx.x >> 5) % QT_WARPS, lane = threadIdx.x & 31;
-  const float scale = 1.4426950408889634f * rsqrtf((float)D);
-  for (int col = 0; col < u.cols; ++col) {
-    const int r = qt_row(a, col), row = u.row0 + r, head = u.h * a.G + col - r * a.G, vis = qt_visible(c, a, u, col);
-    float q[PER], o[PER], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) { q[e] = qc_elem(a.q[(size_t)row * a.q_stride + (size_t)head * D + lane + 32 * e], a.f16); o[e] = 0.f; }
-    for (int t = u.t0 + warp; t < min(u.t1, vis); t += QT_WARPS) {
-      const int id = qc_page(c, u.seq, t >> c.page_log);
-      if (id < 0) continue;
-      const size_t unit = (size_t)id * c.Hkv + u.h;
-      const uint8_t* kp = c.codes + (unit * 2 * c.page + (t & (c.page - 1))) * D;
-      const uint8_t* vp = kp + (size_t)c.page * D;
-      const float2 sc = *reinterpret_cast<const float2*>(c.scales + unit * 2);
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) s += q[e] * (qc_half2(e4m3x2_to_f16x2(kp[lane + 32 * e])).x * sc.x);
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-      s *= scale;
-      const float mn = fmaxf(m, s), corr = m == mn ? 1.f : exp2f(m - mn), p = exp2f(s - mn);
-      l = l * corr + p;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) o[e] = o[e] * corr + p * (qc_half2(e4m3x2_to_f16x2(vp[lane + 32 * e])).x * sc.y);
-      m = mn;
-    }
-#pragma unroll
-    for (int e = 0; e < PER; ++e) smem[warp * ST + lane + 32 * e] = o[e];
-    if (lane == 0) { smem[warp * ST + D] = fmaxf(m, QT_NONE); smem[warp * ST + D + 1] = l; smem[warp * ST + D + 2] = 0.f; }
-    qt_sync(bar);
-    QtUnit one = u;
-    one.cols = 1; one.row0 = row;
-    if (!part) {                                        // qt_write's column 0 is this head
-      QtArgs b = a;
-      b.G = 1; b.Hq = 1; b.by_g = qt_by_g(1);
-      one.row0 = row * a.Hq + head; one.h = 0;
-      qt_write<D>(b, one, smem, 1, nullptr);
-    } else {
-      qt_write<D>(a, one, smem, 1, part + (size_t)col * ST);
-    }
-    qt_sync(bar);
-  }
-}
-
 // A warp per (block of the kernel before, column): joins the parts of the unit that ended in that block's stretch, if it began before.  (A block per
 // column cost the kernel for many rows 38 000 blocks, nearly all without work.)
 template <int D, int COLS, int SLOTS>      // SLOTS: partial results a block has room for

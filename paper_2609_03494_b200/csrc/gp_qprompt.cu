@@ -101,10 +101,11 @@ struct QpShared {
   uint64_t q_full[2], k_full[QP_RING], v_full[QP_RING], k_free[QP_RING], v_free[QP_RING], s_full[2][QP_RING], p_full[2][2], o_full[2][QP_RING];
   uint32_t tmem;
   int dead;                                    // a wait ran out: all others end at once
-  int nan[8];                                  // by the number of the piece: that number, where a value is no number and rows see different tokens
+  int nan[8];                                  // by the number of the piece: that number, where a value that not all rows see is no number
   alignas(16) float ks[2 * QP_RING][QP_N / 16], ev[2 * QP_RING][QP_N / 16];      // per group of 16 tokens: scale of the keys (-1: no such page), exponent of that of the values
   long long x1, share, upto[QP_THREADS], warp[QP_THREADS / 32];
-  float plain[2][QT_WARPS * qt_part(128)], qs[2][QP_M];
+  uint32_t least[8][128];                      // beside nan, per channel: ~piece << 9 | the least row of the tile that sees such a value (an earlier piece's is larger)
+  float qs[2][QP_M];
 };
 // A bounded wait for a phase of a barrier.  (Without a time to suspend for, which brings a second look and a timer to each try: 627 -> 608 us.)
 __device__ __forceinline__ bool qp_try(uint32_t bar, uint32_t parity) {
@@ -237,6 +238,8 @@ struct QpWalk {
 // write them to shared memory as fp16, which holds them exactly and unscaled: K and V in the same image (a token's channels along a row, 64 a
 // swizzled 128 bytes), which the first product reads with the channels, the second with the tokens as inner dimension; four steps of them are there.
 // A warp more for each half issues its products.
+// Values that are no numbers: in steps that not all rows see whole they are put down as 0, with the least row that sees one per channel, whose results (and those of the
+// rows behind) are set at the end.
 // Scales of pages cost nothing per element: 16 columns of S lie in one page, so the keys' scale joins the factor of the logits s and the exponent e of
 // the values' scale the constant that is added before the exponential: p' = 2^(s + e - M), M the running maximum of s + e of the tokens that the row sees.  O is then a plain
 // sum of p' times codes.  The sum of weights has a maximum of its own, m of s: L = sum of 2^(s - m), taken of p' group by group times 2^(M - m - e).  Both are whole
@@ -264,7 +267,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     for (int h = 0; h < 2; ++h) {
       mbar_init(&sh.q_full[h], 4);
       for (int i = 0; i < 2; ++i) mbar_init(&sh.p_full[h][i], 4);
-      for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.s_full[h][i], 2); mbar_init(&sh.o_full[h][i], 1); }
+      for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.s_full[h][i], 2); mbar_init(&sh.o_full[h][i], 2); }
     }
     for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.k_full[i], 1); mbar_init(&sh.v_full[i], 1); mbar_init(&sh.k_free[i], 2); mbar_init(&sh.v_free[i], 2); }
     for (int i = 0; i < 8; ++i) sh.nan[i] = -1;
@@ -272,6 +275,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     fence_mbar_init();
     a.joins[blockIdx.x * 2] = make_int4(0, 0, 0, 0);
   }
+  for (int i = tid; i < 8 * 128; i += QP_THREADS) sh.least[0][i] = ~0u;
   if (warp == QP_ISSUER) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -327,6 +331,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
                 qp_mma_ts(t_o, t_s + (b & 1) * 64 + t * 32 + k * 8, v0 + k * (2048 >> 4), pv, t > 0 || k > 0 ? 1u : (uint32_t)(j > 1));
           }
           qp_commit(o_full + (b & (QP_RING - 1)) * 8);
+          if (lane == 0) qp_arrive(&sh.o_full[half][b & (QP_RING - 1)]);      // hands on, too: which values are no numbers
           qp_commit(v_free + (b & (QP_RING - 1)) * 8);
         }
       }
@@ -383,17 +388,16 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         if (j >= 0) {
         const int s = n + j;
         const int at = s & (QP_RING - 1);
+        bool nan = false;
         if (s >= QP_RING) qp_wait(sh, empty + at, ((s - QP_RING) / QP_RING) & 1);
         if (!kv) {
           const int slot = s & (2 * QP_RING - 1);       // (twice the ring: the weights of a step may still be computed when its keys are replaced)
           if (lane < QP_N / 16) { sh.ks[slot][lane] = sc.x; sh.ev[slot][lane] = (float)((int)((__float_as_uint(sc.y) >> 23) & 255) - 127); }
         } else if (u.t0 + (j + 1) * QP_N > vis0) {      // rows see different tokens of the step
-          bool nan = false;
 #pragma unroll
           for (int i = 0; i < IT; ++i)
             nan |= (__vcmpeq4(r[i].x & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(r[i].y & 0x7f7f7f7f, 0x7f7f7f7f) | __vcmpeq4(r[i].z & 0x7f7f7f7f, 0x7f7f7f7f) |
                     __vcmpeq4(r[i].w & 0x7f7f7f7f, 0x7f7f7f7f)) != 0;
-          if (nan) *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) = piece;
         }
         const uint32_t to = dst + at * OPERAND, to0 = to + at0, to1 = to + at1, odd0 = to + (at0 ^ 64), odd1 = to + (at1 ^ 64);
         qp_each<IT>([&](auto no) {
@@ -403,6 +407,23 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           qp_store16<i * TPI * 128>(odd ? odd0 : to0, e4m3x2_to_f16x2(xa), e4m3x2_hi_to_f16x2(xa), e4m3x2_to_f16x2(ya), e4m3x2_hi_to_f16x2(ya));
           qp_store16<i * TPI * 128>(odd ? odd1 : to1, e4m3x2_to_f16x2(xb), e4m3x2_hi_to_f16x2(xb), e4m3x2_to_f16x2(yb), e4m3x2_hi_to_f16x2(yb));
         });
+        if (__any_sync(0xffffffffu, nan)) {             // values that are no numbers: 0, and who sees them
+          __syncwarp();
+#pragma unroll 1
+          for (int i = lane; i < QP_N * D / 2; i += 32) {      // two channels of a token: [64 channels][token][swizzled piece of 8][pair]
+            const int t = i / 32 % QP_N, c0 = i / (32 * QP_N) * 64 + ((i / 4 % 8) ^ (t & 7)) * 8 + i % 4 * 2;
+            const uint32_t where = v_smem + at * OPERAND + i * 4;
+            uint32_t w;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(where));
+            const uint32_t bad = __vcmpgtu2(w & 0x7fff7fffu, 0x7c007c00u);
+            if (!bad) continue;
+            asm volatile("st.shared.b32 [%0], %1;" ::"r"(where), "r"(w & ~bad) : "memory");
+            const uint32_t key = ~(uint32_t)piece << 9 | (uint32_t)max(u.t0 + j * QP_N + t + 1 - vis0, 0);
+            if (bad & 1) atomicMin(&sh.least[piece & 7][c0], key);
+            if (bad >> 16) atomicMin(&sh.least[piece & 7][c0 + 1], key);
+          }
+          *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) = piece;
+        }
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
@@ -418,7 +439,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     const int half = warp >> 2, t128 = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + T_S + half * 128, t_o = tmem + lanes + T_O + half * 128;
-    const int turn = 3 + (warp & 3) * 2;              // barriers 3 .. 10 (qt_plain has 1 and 2)
+    const int turn = 3 + (warp & 3) * 2;              // barriers 3 .. 10
     if (half) qp_pass(turn);
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
@@ -599,6 +620,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         qp_fence_after();
       }
       if (!used) continue;
+      const bool nan = p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece;
+      const int row = half * RT + qt_row(a, t128);
       float* parts = p.whole ? nullptr : a.part + (size_t)(blockIdx.x * 2 + (p.begins ? 0 : 1)) * QP_COLS * ST + (size_t)half * RT * a.G * ST;
       // by way of the memory of the warp's own 32 queries (no product reads them any more), so that lanes store what lies together
       const uint32_t stage = q_smem + half * QOPERAND + (warp & 3) * (32 * 128);
@@ -622,6 +645,12 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
           }
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = o[e] * inv * scale;
+          if (nan)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint32_t key = sh.least[piece & 7][round * (D / 2) + g * 16 + e];
+              if (key >> 9 == (~(uint32_t)piece & 0x7fffffu) && (int)(key & 511) <= row) o[e] = __int_as_float(0x7fffffff);
+            }
           if (wide) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -663,8 +692,6 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         __syncwarp();
       }
       if (parts && real) *reinterpret_cast<float4*>(parts + (size_t)t128 * ST + D) = make_float4(fmaxf(m, QT_NONE), L, apart, 0.f);
-      if (p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece)      // some row may have met another's NaN: all of the half in plain arithmetic
-        qt_plain<D>(c, a, u, sh.plain[half], parts, 1 + half);
     }
     if (!half) qp_turn(turn);
   }

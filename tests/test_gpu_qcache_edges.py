@@ -229,3 +229,71 @@ def test_values_at_the_upper_end_of_the_range_through_a_list(size):
     pages = rig.gpu.select(rig.batch([1]), q, 500, 1, 1)
     for out in (F32, BF16):
         check_sharp(rig, [1], q64, rig.gpu.attention(rig.batch([1]), q, out_dtype=getattr(T(), out), pages=pages), out, pages.cpu().numpy())
+
+
+# ------------------------------------------------------------------------------------------------ values that are no numbers
+def check_with_nans(rig, s, rows, q64, got, out_dtype, some):
+    """Rows `some` of a sequence's rows against the oracle: NaN where and only where a row sees one, the others within check_attention's bound."""
+    G = q64.shape[1] // rig.heads
+    for i in some:
+        n = int(rig.len[s]) - rows + i + 1
+        for h in range(rig.heads):
+            k, v, _ = rig.ref.rows(rig.table[s], h, n)
+            vmax = np.nanmax(np.abs(v))
+            for g in range(G):
+                q = q64[i, h * G + g]
+                x = k @ q / np.sqrt(rig.d)
+                w = np.exp(x - x.max())
+                ref = (w @ np.nan_to_num(v)) / w.sum()
+                ref[np.isnan(v).any(0)] = np.nan
+                A = float((np.abs(k) @ np.abs(q)).max()) / np.sqrt(rig.d)
+                o = got[i, h * G + g]
+                assert np.array_equal(np.isnan(o), np.isnan(ref)), (s, i, h, g, np.flatnonzero(np.isnan(o) != np.isnan(ref)))
+                if np.isnan(ref).all():
+                    continue
+                tol = 2 * vmax * (rig.d * 2.0 ** -22 * A + 2.0 ** -18) + (0 if out_dtype == F32 else vmax * 2.0 ** -12) + EPS[out_dtype] / 2 * np.abs(ref)
+                ok = np.isnan(ref) | (np.abs(o - ref) <= tol)
+                assert ok.all(), (s, i, h, g)
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8), (64, 3)])
+@pytest.mark.parametrize("rows,held", [(2, 300), (5, 12000), (6, 40), (40, 5000), (200, 7000), (260, 90)])
+def test_values_that_are_no_numbers_reach_the_rows_that_see_them_and_no_others(d, G, rows, held):
+    """In whole units and in those that blocks share (a long sequence with one KV head), in several channels, in rows before the first that is asked for."""
+    rig = Rig(1, 800, 1, d, 16, seed=140 + rows)
+    n = held + rows
+    k, v = rig.draw(n, 1, d), rig.draw(n, 1, d)
+    for back, channels in ((1, [2]), (rows // 2, [7, d - 1]), (rows - 1, [0]), (rows + 1, [9]), (rows + 30, [33])):
+        for c in channels:
+            v[0][n - 1 - back, 0, c] = float("nan" if c % 2 else "inf")
+    rig.append([n], kv=((k[0], f64(k[0])), (v[0], f64(v[0]))))
+    q, q64 = rig.draw(rows, G, d)
+    some = sorted({0, 1, rows // 2 - 1, rows // 2, rows - 2, rows - 1, min(rows - 1, 63), min(rows - 1, 128)} & set(range(rows)))
+    for out in (F32, BF16):
+        got = f64(rig.gpu.attention(rig.batch([rows]), q, out_dtype=getattr(T(), out)))
+        check_with_nans(rig, 0, rows, q64, got, out, some)
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("rows", [4, 30])
+def test_values_that_are_no_numbers_stay_in_their_sequence_and_head(d, G, rows):
+    """Several units a block, those with such values among others."""
+    seqs = 150
+    rig = Rig(seqs, 12, 4, d, 16, seed=150 + rows)
+    lens = [int(x) for x in rig.rng.integers(rows, 180, seqs)]
+    k, v = rig.draw(sum(lens), 4, d), rig.draw(sum(lens), 4, d)
+    at = np.concatenate([[0], np.cumsum(lens)])
+    hit = {}
+    for s in range(0, seqs, 7):
+        h, c, back = s % 4, (5 * s) % d, 1 + s % (rows - 1)
+        v[0][int(at[s + 1]) - 1 - back, h, c] = float("nan")
+        hit[s] = (h, c, back)
+    rig.append(lens, kv=((k[0], f64(k[0])), (v[0], f64(v[0]))))
+    q, q64 = rig.draw(rows * seqs, 4 * G, d)
+    got = f64(rig.gpu.attention(rig.batch([rows] * seqs), q, out_dtype=T().float32)).reshape(seqs, rows, 4, G, d)
+    want = np.zeros(got.shape, bool)
+    for s, (h, c, back) in hit.items():
+        want[s, rows - 1 - back:, h, :, c] = True
+    assert np.array_equal(np.isnan(got), want)
+    for s in (0, 1, 7, 149):
+        check_with_nans(rig, s, rows, q64[s * rows:(s + 1) * rows], got[s].reshape(rows, 4 * G, d), F32, [0, rows - 1])
