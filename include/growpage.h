@@ -554,6 +554,13 @@ int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batch, const vo
                         const int32_t* pages, int32_t n_list, void* out, int32_t out_type, void* work, size_t work_bytes, void* stream);
 size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch, int32_t n_q_heads, int32_t n_list);
 
+/* Test support, like gp_test_withhold: `what` names hand-overs that gp_qcache_attention then does not make (1 the kernel for few rows
+ * of a sequence and lists: the first tiles of the first sequence's first head are never complete; 2 the kernel for many rows: the first keys of
+ * its first thread block are never reported; 0 none), `cycles` is the time after which waits give up (0 = the default, 2^32).  The
+ * thread block concerned sets bit 1 of the status word, issues nothing more and ends; the others are not affected.  Applies to the calls that
+ * the calling thread issues after it. */
+int gp_qcache_test_withhold(int32_t what, int64_t cycles);
+
 /* Chooses the pages that a row's attention over a list looks at, per KV head.  A row sees the pages 0 .. m - 1 up to its
  * own.  Where m <= keep it gets them all; else the `first` first, the `recent` last, and of the others those with
  * the highest

@@ -124,6 +124,7 @@ def lib() -> C.CDLL:
     L.gp_qcache_attention_bytes.argtypes = [qc, qb, i32, i32]; L.gp_qcache_attention_bytes.restype = sz
     L.gp_qcache_select.argtypes = [qc, qb, vp, i64, i32, i32, i32, i32, i32, vp, vp, sz, vp]
     L.gp_qcache_select_bytes.argtypes = [qc, qb]; L.gp_qcache_select_bytes.restype = sz
+    L.gp_qcache_test_withhold.argtypes = [i32, i64]
     _lib = L
     return L
 
@@ -390,6 +391,10 @@ def gp_qcache_select(cache: gp_qcache, batch: gp_qbatch, q_ptr: int, q_stride: i
                      recent: int, pages_ptr: int, work_ptr: int, work_bytes: int, stream: int) -> None:
     _check(lib().gp_qcache_select(C.byref(cache), C.byref(batch), q_ptr, q_stride, n_q_heads, type, keep, first, recent, pages_ptr, work_ptr,
                                   work_bytes, stream), "gp_qcache_select")
+
+
+def gp_qcache_test_withhold(what: int, cycles: int) -> None:
+    _check(lib().gp_qcache_test_withhold(what, cycles), "gp_qcache_test_withhold")
 
 
 # ------------------------------------------------------------------------------- convenience holders

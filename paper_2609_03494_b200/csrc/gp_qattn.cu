@@ -194,7 +194,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     u.t1 = min(LIST ? a.n_list << c.page_log : vis, g1 * QT_GRANULE);
 
     // this warp's tiles: tile j of the warp covers tokens u.t0 + 16 * ((j / QT_TILES * QT_WARPS + warp) * QT_TILES + j % QT_TILES)
-    const int n_stages = (u.t1 - u.t0 + 16 * QT_TILES - 1) / (16 * QT_TILES);
+    const int n_stages = gave_up ? 0 : (u.t1 - u.t0 + 16 * QT_TILES - 1) / (16 * QT_TILES);
     auto tile_token = [&](int j) { return u.t0 + 16 * (((j / QT_TILES) * QT_WARPS + warp) * QT_TILES + j % QT_TILES); };
     // page and scales of 32 of the warp's tiles, a lane each; the next 32 are fetched while these are worked on
     struct Where { int id, tok, left; float ks, vs; };      // page (-1: none), first slot of the tile, slots from it on that some column sees
@@ -235,6 +235,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
     look_scales(cur);
     look_scales(nxt);
 
+    const bool hold = a.withhold & 1 && u.seq == 0 && u.h == 0 && tile == 0 && g0 == 0 && warp == 0;
     auto fetch = [&](int i, int batch) {                // stage i of the warp: lanes 0 .. 3 bring keys and values of its tiles
       if (i * QT_WARPS + warp >= n_stages) return;
       const int j = i * QT_TILES + ((lane >> 1) & (QT_TILES - 1));
@@ -245,9 +246,19 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
       const bool mine = lane < 2 * QT_TILES && left > 0;
       const uint32_t bar = smem_u32(&s_bar[warp][i % STAGES]);
       const int n = __popc(__ballot_sync(0xffffffffu, mine));
-      if (lane == 0) mbar_expect_tx(&s_bar[warp][i % STAGES], n * ROWS);
+      if (lane == 0) mbar_expect_tx(&s_bar[warp][i % STAGES], n * ROWS + (hold && i == 0 ? 16 : 0));
       __syncwarp();
       if (mine) qt_tma_rows(ring + (i % STAGES) * STAGE + lane * ROWS, &map, (u.h * 2 + (lane & 1)) * c.page + (tok & (c.page - 1)), id, bar);
+    };
+    auto arrived = [&](int i) {                         // a bounded wait of the warp for stage i
+      uint64_t* bar = &s_bar[warp][i % STAGES];
+      const uint32_t parity = (phases >> (i % STAGES)) & 1;
+      phases ^= 1u << (i % STAGES);
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+      const long long since = clock64();
+      while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)))
+        if (__any_sync(0xffffffffu, clock64() - since > a.patience)) return false;
+      return true;
     };
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) fetch(i, 0);
@@ -320,11 +331,10 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
         look_scales(nxt);
       }
       fetch(i + STAGES - 1, batch);
-      {
-        const int st = i % STAGES;
-        for (unsigned spin = 0; !mbar_try_wait(&s_bar[warp][st], (phases >> st) & 1); ++spin)
-          if (spin > GP_SPIN_LIMIT) { gave_up = true; break; }
-        phases ^= 1u << st;
+      if (!arrived(i)) {                                // nothing more is asked for; what has been is waited for before the memory is anything else's
+        gave_up = true;
+        for (int k = i + 1; k < i + STAGES && k * QT_WARPS + warp < n_stages; ++k) arrived(k);
+        break;
       }
       const uint32_t stage = ring + (i % STAGES) * STAGE;
       int left[QT_TILES], tok[QT_TILES];
@@ -598,6 +608,14 @@ QtBoth qt_both(const QcDev& c, int G, int d, int n_list) {
 
 }  // namespace
 
+static thread_local struct { long long patience; int withhold; } qt_test = {QT_PATIENCE, 0};
+
+extern "C" int gp_qcache_test_withhold(int32_t what, int64_t cycles) {
+  if (what < 0 || what > 3 || cycles < 0) return GP_ERR_INVALID;
+  qt_test = {cycles > 0 ? cycles : QT_PATIENCE, what};
+  return GP_OK;
+}
+
 extern "C" size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch, int32_t n_q_heads, int32_t n_list) {
   QcDev c;
   if (qc_check(cache, batch, &c) != GP_OK || n_q_heads < 1 || n_q_heads % c.Hkv || n_q_heads / c.Hkv > 8 || n_list < 0) return 0;
@@ -621,6 +639,7 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
   a.out = out; a.out_type = out_type;
   const int d = cache->head_dim;
   a.few = qt_few(d);
+  a.patience = qt_test.patience; a.withhold = qt_test.withhold;
   const QtBoth b = qt_both(c, a.G, d, n_list);
   if (!work || qc_misaligned(work, 16) || work_bytes < b.bytes) return GP_ERR_INVALID;
   QcDevice dev(cache->device);

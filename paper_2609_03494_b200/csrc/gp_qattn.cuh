@@ -29,7 +29,10 @@ struct QtArgs {
   int few;                                     // qt_few
   unsigned by_g;                               // qt_row
   int rows_tile;                               // rows whose columns (row, query head of the group) a thread block has together
+  long long patience;                          // cycles after which a wait gives up
+  int withhold;                                // gp_qcache_test_withhold
 };
+constexpr long long QT_PATIENCE = 1ll << 32;   // 2 s
 
 __device__ __forceinline__ float qt_exp2(float x) {      // 2^x to 2^-22 relative; 0 below 2^-126
   float y;

@@ -8,7 +8,6 @@ namespace {
 constexpr int QP_M = 128;                      // columns (row, query head of the group) of a half of a block's tile: the rows of a product
 constexpr int QP_COLS = 2 * QP_M;
 constexpr int QP_N = 64;                       // tokens of a step
-constexpr long long QP_PATIENCE = 1ll << 32;   // cycles (2 s) after which a wait gives up
 constexpr int QP_RING = 4;                     // steps whose keys and values there is room for
 constexpr int QP_SOFT = 256;                   // threads that turn logits into weights, a column each (warps 0 .. 7)
 constexpr int QP_TURN = 3;                     // warps that turn keys into fp16, a step each in turn (8 .. 10); as many turn values (11 .. 13)
@@ -65,7 +64,7 @@ template <int N, class F>
 __device__ __forceinline__ void qp_each(F&& f) { qp_each_of(f, std::make_integer_sequence<int, N>{}); }
 // The two warps of weights of a scheduler (one of each half) take turns at the exponentials, so that one's wait, logits and maximum fall into the other's
 // turn; left to themselves they run in step or not by chance (chunks of 32 768 tokens 608 to 657 us; 579 so).  Both make a turn of each step of a piece
-// whether the half is used or not, and all their other waits are bounded: every turn comes.
+// whether the half is used or not, and whether a wait gave up or not, and all their other waits are bounded: every turn comes.
 __device__ __forceinline__ void qp_turn(int id) { __syncwarp(); asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void qp_pass(int id) { __syncwarp(); asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
 // 32, 16, 8 columns of the warp's 32 lanes
@@ -98,16 +97,16 @@ __device__ __forceinline__ void qp_st16(uint32_t t, const uint32_t* r) {
 
 struct QpShared {
   // [half], and by the place of the step in its ring
-  uint64_t q_full[2], k_full[QP_RING], v_full[QP_RING], k_free[QP_RING], v_free[QP_RING], s_full[2][QP_RING], p_full[2][2], o_full[2][QP_RING];
+  uint64_t q_full[2], k_full[QP_RING], v_full[QP_RING], k_free[QP_RING], v_free[QP_RING], s_full[2][QP_RING], p_full[2][2], o_full[2][QP_RING], end[2];
   uint32_t tmem;
-  int dead;                                    // a wait ran out: all others end at once
+  int dead;                                    // a wait ran out: all others do at once
   int nan[8];                                  // by the number of the piece: that number, where a value that not all rows see is no number
   alignas(16) float ks[2 * QP_RING][QP_N / 16], ev[2 * QP_RING][QP_N / 16];      // per group of 16 tokens: scale of the keys (-1: no such page), exponent of that of the values
   long long x1, share, upto[QP_THREADS], warp[QP_THREADS / 32];
   uint32_t least[8][128];                      // beside nan, per channel: ~piece << 9 | the least row of the tile that sees such a value (an earlier piece's is larger)
   float qs[2][QP_M];
 };
-// A bounded wait for a phase of a barrier.  (Without a time to suspend for, which brings a second look and a timer to each try: 627 -> 608 us.)
+// (Without a time to suspend for, which brings a second look and a timer to each try: 627 -> 608 us.)
 __device__ __forceinline__ bool qp_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
@@ -119,13 +118,17 @@ __device__ __forceinline__ bool qp_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ void qp_wait(QpShared& sh, uint64_t* bar, uint32_t parity) {
+__device__ __forceinline__ void qp_wait(QpShared& sh, const QtArgs& a, uint64_t* bar, uint32_t parity) {
   const uint32_t at = smem_u32(bar);
   if (qp_try(at, parity)) return;
   const long long since = clock64();
   while (!qp_try(at, parity))
-    if (clock64() - since > QP_PATIENCE || *reinterpret_cast<volatile int*>(&sh.dead)) { *reinterpret_cast<volatile int*>(&sh.dead) = 1; break; }
+    if (clock64() - since > a.patience || *reinterpret_cast<volatile int*>(&sh.dead)) { *reinterpret_cast<volatile int*>(&sh.dead) = 1; break; }
 }
+// Whether no wait of the block has given up; the same in all lanes.  In a block with one that has, all waits end at once: its warps that issue products leave at the next step
+// and wait for what they issued, the others go through the rest of their steps and turns with whatever lies there, and no result is written.  (Asked for behind each wait
+// of the issuing warps: chunks 218 us for 214; by the warps that convert 4 more, by those of weights 7.)
+__device__ __forceinline__ bool qp_alive(const QpShared& sh) { return !__any_sync(0xffffffffu, *reinterpret_cast<const volatile int*>(&sh.dead)); }
 
 // The line of work (as in the other kernel): sequence by sequence, KV head by KV head, tile of rows by tile of rows, measured in tokens.  Tile t of
 // a sequence has s + R (t + 1) + QP_UNIT of it, with R the rows of a tile and s the slot of the sequence's first row, so T tiles have
@@ -265,7 +268,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
 
   if (tid == 0) {
     for (int h = 0; h < 2; ++h) {
-      mbar_init(&sh.q_full[h], 4);
+      mbar_init(&sh.q_full[h], 4); mbar_init(&sh.end[h], 1);
       for (int i = 0; i < 2; ++i) mbar_init(&sh.p_full[h][i], 4);
       for (int i = 0; i < QP_RING; ++i) { mbar_init(&sh.s_full[h][i], 2); mbar_init(&sh.o_full[h][i], 2); }
     }
@@ -298,14 +301,15 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
                    k_free = smem_u32(sh.k_free), v_free = smem_u32(sh.v_free);
     int4 join[2];
     join[0].x = 0;
-    for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
+    bool ok = true;
+    for (int piece = 0; ok && walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       const int steps = __shfl_sync(0xffffffffu, p.n_steps, 0), n0 = __shfl_sync(0xffffffffu, n, 0);
       const bool used = __shfl_sync(0xffffffffu, (int)(half == 0 || p.u.cols > RT * a.G), 0);
-      if (steps > 0) qp_wait(sh, &sh.q_full[half], piece & 1);
-      for (int j = 0; j <= steps; ++j) {                // the next logits, then the product with the weights of the step before
+      if (steps > 0) qp_wait(sh, a, &sh.q_full[half], piece & 1);
+      for (int j = 0; j <= steps && (ok = qp_alive(sh)); ++j) {                // the next logits, then the product with the weights of the step before
         const uint32_t s = n0 + j;
         if (j < steps) {
-          qp_wait(sh, &sh.k_full[s & (QP_RING - 1)], (s / QP_RING) & 1);
+          qp_wait(sh, a, &sh.k_full[s & (QP_RING - 1)], (s / QP_RING) & 1);
           qp_fence_after();
           if (used) {
             const uint64_t k0 = dk + (s & (QP_RING - 1)) * (OPERAND >> 4);
@@ -319,8 +323,8 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         }
         if (j > 0) {
           const uint32_t b = s - 1;
-          qp_wait(sh, &sh.v_full[b & (QP_RING - 1)], (b / QP_RING) & 1);
-          qp_wait(sh, &sh.p_full[half][b & 1], (b >> 1) & 1);
+          qp_wait(sh, a, &sh.v_full[b & (QP_RING - 1)], (b / QP_RING) & 1);
+          qp_wait(sh, a, &sh.p_full[half][b & 1], (b >> 1) & 1);
           qp_fence_after();
           if (used) {
             const uint64_t v0 = dv + (b & (QP_RING - 1)) * (OPERAND >> 4);
@@ -337,7 +341,11 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       }
       n += p.n_steps;
     }
-    if (warp == QP_ISSUER && lane == 0 && join[0].x > 0) { a.joins[blockIdx.x * 2] = join[0]; a.joins[blockIdx.x * 2 + 1] = join[1]; }
+    qp_commit(smem_u32(&sh.end[half]));                 // all that was issued: before the tensor memory is given back and the block's shared memory ends
+    const long long since = clock64();
+    while (!__all_sync(0xffffffffu, qp_try(smem_u32(&sh.end[half]), 0)))
+      if (__any_sync(0xffffffffu, clock64() - since > QT_PATIENCE)) { *reinterpret_cast<volatile int*>(&sh.dead) = 1; break; }
+    if (ok && warp == QP_ISSUER && lane == 0 && join[0].x > 0) { a.joins[blockIdx.x * 2] = join[0]; a.joins[blockIdx.x * 2 + 1] = join[1]; }
   } else if (warp >= 8) {                               // ---- codes to fp16: three warps the keys, three the values, a step each in turn
     const int kv = (warp - 8) / QP_TURN, turn = (warp - 8) % QP_TURN;
     constexpr int TPI = 32 / CH;                        // tokens of a round: 4 or 8
@@ -349,6 +357,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     const size_t page_bytes = (size_t)c.Hkv * 2 * c.page * D;
     const uint32_t full = smem_u32(kv ? sh.v_full : sh.k_full);
     uint64_t* empty = kv ? sh.v_free : sh.k_free;       // both halves' products have read what was there
+    const bool hold = a.withhold & 2 && blockIdx.x == 0 && !kv;
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       const QtUnit& u = p.u;
@@ -389,7 +398,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         const int s = n + j;
         const int at = s & (QP_RING - 1);
         bool nan = false;
-        if (s >= QP_RING) qp_wait(sh, empty + at, ((s - QP_RING) / QP_RING) & 1);
+        if (s >= QP_RING) qp_wait(sh, a, empty + at, ((s - QP_RING) / QP_RING) & 1);
         if (!kv) {
           const int slot = s & (2 * QP_RING - 1);       // (twice the ring: the weights of a step may still be computed when its keys are replaced)
           if (lane < QP_N / 16) { sh.ks[slot][lane] = sc.x; sh.ev[slot][lane] = (float)((int)((__float_as_uint(sc.y) >> 23) & 255) - 127); }
@@ -426,7 +435,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         }
         fence_proxy_async();
         __syncwarp();
-        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
+        if (lane == 0 && !(hold && s == 0)) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(full + at * 8) : "memory");
         }
         if (j + QP_TURN < p.n_steps) {
           load(j + QP_TURN, next);
@@ -441,6 +450,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
     const uint32_t t_s = tmem + lanes + T_S + half * 128, t_o = tmem + lanes + T_O + half * 128;
     const int turn = 3 + (warp & 3) * 2;              // barriers 3 .. 10
     if (half) qp_pass(turn);
+    bool ok = true;
     int4 join[2];
     for (int piece = 0; walk.next(c, a, R, sh, p, join); piece += p.n_steps > 0) {
       QtUnit u = p.u;                                   // of this half
@@ -451,7 +461,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       const int see = real ? qt_visible(c, a, u, t128) : 0x7fffffff;
       const int least = __reduce_min_sync(0xffffffffu, see);
       float qs = 0.f;                                   // what S is multiplied with
-      if (used && p.n_steps > 0) {                      // the warp's 32 columns, D / 8 lanes a column
+      if (used && ok && p.n_steps > 0) {                // the warp's 32 columns, D / 8 lanes a column
         constexpr int LPC = D / 8, CPR = 32 / LPC, ROUNDS = 32 / CPR;
         const int piece8 = lane % LPC;
         int col = (warp & 3) * 32 + lane / LPC;
@@ -507,7 +517,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       for (int j = 0; j < p.n_steps; ++j) {
         const int s = n + j;
         const int slot = s & (2 * QP_RING - 1);
-        qp_wait(sh, &sh.s_full[half][s & (QP_RING - 1)], (s / QP_RING) & 1);
+        qp_wait(sh, a, &sh.s_full[half][s & (QP_RING - 1)], (s / QP_RING) & 1);
         qp_fence_after();
         if (used) {
           const uint32_t t_x = t_s + (s & 1) * 64;
@@ -561,7 +571,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
               M = to; m = top;
             }
             if (j > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
-              qp_wait(sh, &sh.o_full[half][(s - 1) & (QP_RING - 1)], ((s - 1) / QP_RING) & 1);      // all of O is there
+              qp_wait(sh, a, &sh.o_full[half][(s - 1) & (QP_RING - 1)], ((s - 1) / QP_RING) & 1);      // all of O is there
               qp_fence_after();
 #pragma unroll 1
               for (int g = 0; g < D / 16; ++g) {
@@ -615,11 +625,12 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         if (lane == 0) qp_arrive(&sh.p_full[half][s & 1]);
       }
       n += p.n_steps;
-      if (p.n_steps > 0) {
-        qp_wait(sh, &sh.o_full[half][(n - 1) & (QP_RING - 1)], ((n - 1) / QP_RING) & 1);
+      if (ok && p.n_steps > 0) {
+        qp_wait(sh, a, &sh.o_full[half][(n - 1) & (QP_RING - 1)], ((n - 1) / QP_RING) & 1);
+        ok = qp_alive(sh);
         qp_fence_after();
       }
-      if (!used) continue;
+      if (!used || !ok) continue;
       const bool nan = p.n_steps > 0 && *reinterpret_cast<volatile int*>(&sh.nan[piece & 7]) == piece;
       const int row = half * RT + qt_row(a, t128);
       float* parts = p.whole ? nullptr : a.part + (size_t)(blockIdx.x * 2 + (p.begins ? 0 : 1)) * QP_COLS * ST + (size_t)half * RT * a.G * ST;

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from paper_2609_03494_b200 import binding as B
 from tests.test_gpu_qcache import BF16, EPS, F32, Rig, T, dev, f64
 
 pytestmark = pytest.mark.gpu
@@ -297,3 +298,34 @@ def test_values_that_are_no_numbers_stay_in_their_sequence_and_head(d, G, rows):
     assert np.array_equal(np.isnan(got), want)
     for s in (0, 1, 7, 149):
         check_with_nans(rig, s, rows, q64[s * rows:(s + 1) * rows], got[s].reshape(rows, 4 * G, d), F32, [0, rows - 1])
+
+
+# ------------------------------------------------------------------------------------------------ waits that run out
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("what,rows,listed", [(1, 1, False), (1, 3, False), (1, 1, True), (2, 60, False), (2, 300, False)])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_as_before(d, G, what, rows, listed):
+    """One hand-over is not made (never signalled, nothing faults): the waits of its thread block give up after 200 000 cycles, the block ends, the status word says so;
+    blocks of other sequences are not affected."""
+    torch = T()
+    rig = Rig(6, 80, 2, d, 16, seed=160)
+    rig.append([900, 30, 700, 400, 650, 880 - rows])
+    rig.append([rows] * 6)
+    q, q64 = rig.draw(6 * rows, 2 * G, d)
+    b = rig.batch([rows] * 6)
+    pages = rig.gpu.select(b, q, 20, 1, 1) if listed else None
+    call = lambda: rig.gpu.attention(b, q, out=torch.full(q.shape, 9.0, device="cuda"), pages=pages)  # noqa: E731
+    want = call()
+    torch.cuda.synchronize()
+    assert int(rig.status.item()) == 0
+    B.gp_qcache_test_withhold(what, 200000)
+    try:
+        got = call()
+        torch.cuda.synchronize()
+    finally:
+        B.gp_qcache_test_withhold(0, 0)
+    assert int(rig.status.item()) == 1
+    assert torch.equal(got[-rows:], want[-rows:])
+    rig.status.zero_()
+    for _ in range(3):
+        assert torch.equal(call(), want)
+    assert int(rig.status.item()) == 0

@@ -107,3 +107,9 @@ def test_structs_match_the_header():
         body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (name, name), text, flags=re.S).group(1)
         fields = [n.strip(" *") for decl in body.split(";") if decl.strip() for n in re.sub(r"^\s*(const\s+)?\w+", "", decl).split(",")]
         assert fields == [f[0] for f in getattr(B, name)._fields_], name
+
+
+def test_withheld_hand_overs_are_numbered():
+    for what, cycles in ((-1, 0), (4, 0), (1, -1)):
+        assert B.lib().gp_qcache_test_withhold(what, cycles) == B.GP_ERR_INVALID
+    assert B.lib().gp_qcache_test_withhold(0, 0) == B.GP_OK
