@@ -558,8 +558,8 @@ class QCache:
         stride, head, elem = t.stride()
         if elem != 1 or (head != self.head_dim and t.shape[1] > 1):
             raise ValueError(f"{name}: the heads of a row lie one behind the other")
-        if batch.n_rows <= 1:
-            stride = max(stride, t.shape[1] * self.head_dim)
+        if batch.n_rows <= 1:                              # (a distance that nothing is at)
+            stride = t.shape[1] * self.head_dim
         if len(self._checked) > 1000:
             self._checked.clear()
         self._checked[key] = stride
