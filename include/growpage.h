@@ -532,7 +532,9 @@ typedef struct gp_qrows {
 
 /* Puts the batch's rows into the cache: normalised (optional), rotated (optional), in e4m3, with the scales and, where
  * the cache has them, the bounds of the pages they touch; the queries with them.  Keys are computed in fp64 (their
- * largest magnitude decides the scale's exponent), queries in fp32, rounded once.  k, v, q, q_out 16-byte aligned;
+ * largest magnitude decides the scale's exponent), queries in fp32, rounded once (the sum of a query head's squares, too: heads
+ * whose mean square plus eps lies outside fp32's normal numbers, 2^-126 to 2^128, are not normalised rightly).  Rows that lie in no slot
+ * below max_len (or below 0) leave nothing in the cache, and their q_out as it was.  k, v, q, q_out 16-byte aligned;
  * a page that receives rows must belong to one sequence of the batch only.  Sequences by themselves may have their
  * rows appended again: the same codes result.  Asynchronous on `stream`, no workspace; can be captured. */
 int gp_qcache_append(const gp_qcache* cache, const gp_qbatch* batch, const gp_qrows* rows, void* stream);
