@@ -542,6 +542,11 @@ class QCache:
     def stream(self) -> int:
         return self._raw_stream(self._index)
 
+    def _no_grad(self, *tensors) -> None:
+        """Nothing of a gradient passes through the cache: a tensor that wants one is refused rather than cut off."""
+        if self.torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+            raise ValueError("the 8-bit cache has no backward pass: call it under torch.no_grad(), or with tensors that require no gradient")
+
     def _rows(self, name: str, t, batch: QBatch, heads: int, dtype=None) -> int:
         """Checks a [n_rows][heads][head_dim] tensor whose rows may be apart; returns the distance between them.  (Checked once per
         shape, strides and type: the checks cost as much as a launch.)"""
@@ -568,8 +573,9 @@ class QCache:
     def append(self, batch: QBatch, k, v, q=None, q_out=None, positions=None, rope_theta: float = 0.0, q_weight=None, k_weight=None,
                eps: float = 1e-6):
         """Puts the batch's rows into the cache (gp_qcache_append); returns the normalised and rotated queries (q_out, a new tensor where
-        none is given), or None without q."""
+        none is given, whose rows that are no sequence's or lie in no slot below max_len are not written), or None without q.  No gradients."""
         torch = self.torch
+        self._no_grad(k, v, q, q_weight, k_weight)
         dtype = k.dtype
         ks, vs = self._rows("k", k, batch, self.n_kv_heads), self._rows("v", v, batch, self.n_kv_heads, dtype)
         for name, t, kind, n in (("positions", positions, torch.int32, batch.n_rows), ("q_weight", q_weight, torch.float32, self.head_dim),
@@ -593,8 +599,10 @@ class QCache:
         return q_out
 
     def attention(self, batch: QBatch, q, out=None, out_dtype=None, pages=None):
-        """Attention of the batch's rows (gp_qcache_attention): all pages, or pages int32 [n_rows][n_kv_heads][n_list]."""
+        """Attention of the batch's rows (gp_qcache_attention): all pages, or pages int32 [n_rows][n_kv_heads][n_list].  A result tensor that is not
+        given is new, and rows that are no sequence's, or beyond max_rows of one, are not written.  No gradients."""
         torch = self.torch
+        self._no_grad(q)
         stride = self._rows("q", q, batch, 0)
         if out is None:
             out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
@@ -623,6 +631,7 @@ class QCache:
     def select(self, batch: QBatch, q, keep: int, first: int = 1, recent: int = 1, pages=None):
         """The pages a row looks at per KV head (gp_qcache_select): int32 [n_rows][n_kv_heads][keep], ascending, -1 behind the last."""
         torch = self.torch
+        self._no_grad(q)
         stride = self._rows("q", q, batch, 0)
         shape = (batch.n_rows, self.n_kv_heads, keep)
         if pages is None:

@@ -29,3 +29,18 @@ def test_a_single_row_has_no_distance_to_another(width):
     q = torch.zeros(2, width, dtype=torch.bfloat16)[:, :4 * 64].view(2, 4, 64)[:1]
     assert q.stride(0) == width
     assert holder()._rows("q", q, Batch(1), 4) == 4 * 64
+
+
+def test_tensors_that_want_a_gradient_are_refused():
+    c = holder()
+    c.n_kv_heads = 2
+    t = lambda heads, grad=False: torch.zeros(3, heads, 64, dtype=torch.bfloat16, requires_grad=grad)  # noqa: E731
+    w = torch.ones(64, requires_grad=True)
+    for kw in (dict(k=t(2, True)), dict(v=t(2, True)), dict(q=t(4, True)), dict(q=t(4), q_weight=w), dict(k_weight=w)):
+        with pytest.raises(ValueError, match="no backward"):
+            c.append(Batch(3), **{"k": t(2), "v": t(2), **kw})
+    for call in (c.attention, lambda b, q: c.select(b, q, 4)):
+        with pytest.raises(ValueError, match="no backward"):
+            call(Batch(3), t(4, True))
+    with torch.no_grad():
+        c._no_grad(t(2, True), None, w)                   # (the same tensors where no gradients are recorded)
