@@ -542,6 +542,13 @@ class QCache:
     def stream(self) -> int:
         return self._raw_stream(self._index)
 
+    def status_bits(self) -> int:
+        """What the kernels have reported so far (gp_qcache.status: 4 a page id that is none of the cache's, 1 a bounded wait that gave up); waits for the
+        current stream.  The bits stay until the caller clears the tensor."""
+        if self.tensors[3] is None:
+            raise ValueError("a cache without a status tensor is told nothing")
+        return int(self.tensors[3].item())
+
     def _no_grad(self, *tensors) -> None:
         """Nothing of a gradient passes through the cache: a tensor that wants one is refused rather than cut off."""
         if self.torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):

@@ -44,3 +44,12 @@ def test_tensors_that_want_a_gradient_are_refused():
             call(Batch(3), t(4, True))
     with torch.no_grad():
         c._no_grad(t(2, True), None, w)                   # (the same tensors where no gradients are recorded)
+
+
+def test_the_status_word_can_be_asked_for():
+    c = holder()
+    c.tensors = (None, None, None, torch.tensor([4], dtype=torch.int32))
+    assert c.status_bits() == 4
+    c.tensors = (None, None, None, None)
+    with pytest.raises(ValueError):
+        c.status_bits()
