@@ -504,7 +504,7 @@ typedef struct gp_qbatch {
   int32_t n_seq, table_stride;
   int32_t n_rows;            /* rows of the tensors                                                                    */
   int32_t max_rows;          /* rows of one sequence at most                                                           */
-  int32_t max_len;           /* tokens of one sequence at most                                                         */
+  int32_t max_len;           /* tokens of one sequence at most (2^31 - 2^16; the pages of a table's row bound it, too) */
   int32_t reserved;          /* keep 0                                                                                 */
 } gp_qbatch;
 

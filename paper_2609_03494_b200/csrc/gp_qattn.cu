@@ -629,7 +629,7 @@ extern "C" int gp_qcache_attention(const gp_qcache* cache, const gp_qbatch* batc
   if (st != GP_OK) return st;
   if (!qc_check_q(cache, q, q_stride, n_q_heads, type) || qc_misaligned(out, 16) || (!qc_empty(c) && (!q || !out))) return GP_ERR_INVALID;
   if (out_type != GP_TYPE_BF16 && out_type != GP_TYPE_F16 && out_type != GP_TYPE_F32) return GP_ERR_INVALID;
-  if (pages ? n_list < 1 || qc_misaligned(pages, 4) || (long long)n_list * c.page > 0x7fffff00 : n_list != 0) return GP_ERR_INVALID;
+  if (pages ? n_list < 1 || qc_misaligned(pages, 4) || (long long)n_list * c.page > QC_MAX_LEN : n_list != 0) return GP_ERR_INVALID;
   if (qc_empty(c)) return GP_OK;
   QtArgs a;
   a.q = static_cast<const unsigned short*>(q);

@@ -13,6 +13,8 @@
 #define QC_E_MIN (-117)        // the smallest code 2^-9 in the smallest scale is the smallest normal fp32 and bf16 number
 #define QC_E_MAX 119           // 448 * 2^119 is the largest code times a power of two that fp32 holds
 
+#define QC_MAX_LEN 0x7fff0000  // slots, and places of a list times the page size: what is added to them on the way stays below 2^31
+
 struct QcDev {                 // a gp_qcache and a gp_qbatch as the kernels take them
   uint8_t* codes;
   float* scales;
@@ -138,6 +140,7 @@ inline int qc_check(const gp_qcache* c, const gp_qbatch* b, QcDev* d) {
   d->n_seq = b->n_seq; d->stride = b->table_stride; d->n_rows = b->n_rows;
   d->max_rows = b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
   const long long room = (long long)b->table_stride * c->page_size;
+  if (room > QC_MAX_LEN && b->max_len > QC_MAX_LEN) return GP_ERR_TOO_LARGE;
   d->limit = room < b->max_len ? (int)room : b->max_len;
   return GP_OK;
 }

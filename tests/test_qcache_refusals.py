@@ -113,3 +113,16 @@ def test_withheld_hand_overs_are_numbered():
     for what, cycles in ((-1, 0), (4, 0), (1, -1)):
         assert B.lib().gp_qcache_test_withhold(what, cycles) == B.GP_ERR_INVALID
     assert B.lib().gp_qcache_test_withhold(0, 0) == B.GP_OK
+
+
+@pytest.mark.parametrize("call", [append, attention, select])
+def test_slots_that_would_pass_31_bits_are_refused(call):
+    """A table of 2^31 tokens with a bound as large: indexes are added up in 32 bits."""
+    assert call(cache=_cache(page_size=256), batch=_batch(table_stride=1 << 23, max_len=(1 << 31) - 1)) == B.GP_ERR_TOO_LARGE
+    assert call(cache=_cache(page_size=256), batch=_batch(table_stride=1 << 24, max_len=(1 << 31) - (1 << 16) + 1)) == B.GP_ERR_TOO_LARGE
+
+
+def test_lists_that_would_pass_31_bits_are_refused():
+    c = _cache(page_size=256)
+    assert attention(cache=c, pages=A, n_list=(1 << 23) - 255) == B.GP_ERR_INVALID
+    assert B.gp_qcache_attention_bytes(c, _batch(), 32, (1 << 23) - 256) > 0
