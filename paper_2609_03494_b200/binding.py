@@ -628,7 +628,7 @@ class QCache:
         key = (self._shape, heads, n_list)
         need = batch.work.get(key)
         if need is None:
-            need = batch.work[key] = self._lib.gp_qcache_attention_bytes(self._ref, batch.ref, heads, n_list)
+            need = batch.work[key] = gp_qcache_attention_bytes(self.desc, batch.desc, heads, n_list)
         work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         _check(self._lib.gp_qcache_attention(self._ref, batch.ref, q.data_ptr(), stride, heads, self._types[q.dtype], pages_ptr, n_list,
                                              out.data_ptr(), out_type, work.data_ptr() if need else None, need,
@@ -648,7 +648,7 @@ class QCache:
         key = (self._shape, "select")
         need = batch.work.get(key)
         if need is None:
-            need = batch.work[key] = self._lib.gp_qcache_select_bytes(self._ref, batch.ref)
+            need = batch.work[key] = gp_qcache_select_bytes(self.desc, batch.desc)
         work = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         _check(self._lib.gp_qcache_select(self._ref, batch.ref, q.data_ptr(), stride, q.shape[1], self._types[q.dtype], keep, first, recent,
                                           pages.data_ptr(), work.data_ptr() if need else None, need, self._raw_stream(self._index)),

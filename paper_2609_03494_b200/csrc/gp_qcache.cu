@@ -637,7 +637,7 @@ __device__ __forceinline__ float qc_unkey(uint32_t k) { return __uint_as_float(k
 
 struct QsShared {
   int hist[1 << QS_BITS];
-  int seq, bin, left, count, close, page[QS_CLOSE];
+  int seq, bin, left, count, page[QS_CLOSE];
   unsigned long long lo[QS_SEL_THREADS / 32], hi[QS_SEL_THREADS / 32], sum[QS_SEL_THREADS / 32], key[QS_CLOSE];
   float err[QS_SEL_THREADS / 32];
 };
@@ -750,7 +750,6 @@ qc_select_kernel(const __grid_constant__ QcDev c, const unsigned short* __restri
   for (int i = tid; i < recent; i += QS_SEL_THREADS) out[keep - recent + i] = m - recent + i;
   const int want = keep - first - recent, n = m - first - recent;        // want < n
   for (int i = tid; i < 1 << QS_BITS; i += QS_SEL_THREADS) sh.hist[i] = 0;
-  if (tid == 0) sh.close = 0;
   gp_pdl_wait();
   if (want == 0) return;
   float2* src = scores + (size_t)unit * key_stride + first;

@@ -329,3 +329,29 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_as_before(d, G, w
     for _ in range(3):
         assert torch.equal(call(), want)
     assert int(rig.status.item()) == 0
+
+
+# ------------------------------------------------------------------------------------------------ without the holder
+def test_the_calls_of_the_c_interface_are_those_of_the_holder():
+    torch = T()
+    a, b = Rig(2, 30, 2, 64, 16, seed=180), Rig(2, 30, 2, 64, 16, seed=180)
+    for rig in (a, b):
+        rig.append([300, 41])
+        rig.len = rig.len + 2
+    batch, stream = a.batch([2, 2]), a.gpu.stream()
+    q, k, v = (a.draw(4, n, 64)[0] for n in (8, 2, 2))
+    want_q = a.gpu.append(batch, k, v, q=q, rope_theta=1e4)
+    want_pages = a.gpu.select(batch, want_q, 5, 1, 1)
+    want = a.gpu.attention(batch, want_q, pages=want_pages, out_dtype=torch.float32)
+    batch = b.batch([2, 2])
+    got_q, got_pages, got = torch.empty_like(want_q), torch.empty_like(want_pages), torch.empty_like(want)
+    rows = B.gp_qrows(k=k.data_ptr(), v=v.data_ptr(), q=q.data_ptr(), q_out=got_q.data_ptr(), k_stride=128, v_stride=128, q_stride=512, q_out_stride=512,
+                      rope_theta=1e4, n_q_heads=8, type=B.GP_TYPE_BF16)
+    B.gp_qcache_append(b.gpu.desc, batch.desc, rows, stream)
+    sizes = [B.gp_qcache_select_bytes(b.gpu.desc, batch.desc), B.gp_qcache_attention_bytes(b.gpu.desc, batch.desc, 8, 5)]
+    work = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    B.gp_qcache_select(b.gpu.desc, batch.desc, got_q.data_ptr(), 512, 8, B.GP_TYPE_BF16, 5, 1, 1, got_pages.data_ptr(), work[0].data_ptr(), sizes[0], stream)
+    B.gp_qcache_attention(b.gpu.desc, batch.desc, got_q.data_ptr(), 512, 8, B.GP_TYPE_BF16, got_pages.data_ptr(), 5, got.data_ptr(), B.GP_TYPE_F32,
+                          work[1].data_ptr(), sizes[1], stream)
+    assert torch.equal(got_q, want_q) and torch.equal(got_pages, want_pages) and torch.equal(got, want)
+    assert torch.equal(a.codes.view(torch.uint8), b.codes.view(torch.uint8)) and torch.equal(a.bounds.view(torch.uint8), b.bounds.view(torch.uint8))
