@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from paper_2609_03494_b200 import binding as B
-from tests.test_gpu_qcache import BF16, EPS, F32, Rig, T, dev, f64
+from tests.test_gpu_qcache import BF16, EPS, F32, Rig, T, check_attention, dev, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -355,3 +355,15 @@ def test_the_calls_of_the_c_interface_are_those_of_the_holder():
                           work[1].data_ptr(), sizes[1], stream)
     assert torch.equal(got_q, want_q) and torch.equal(got_pages, want_pages) and torch.equal(got, want)
     assert torch.equal(a.codes.view(torch.uint8), b.codes.view(torch.uint8)) and torch.equal(a.bounds.view(torch.uint8), b.bounds.view(torch.uint8))
+
+
+@pytest.mark.parametrize("d,page,dtype", [(64, 16, BF16), (128, 16, "float16"), (128, 64, BF16), (64, 128, "float16"), (128, 256, BF16)])
+def test_a_cache_without_bounds(d, page, dtype):
+    rig = Rig(3, 3 + 200 // page, 5, d, page, seed=190 + d, bounds=False)
+    for rows, scale in (([page + 3, 0, 1], 1.0), ([1, 1, 1], 30.0), ([5, 2, 17], 0.1), ([page, page - 1, 0], 1e3), ([1, 1, 2], 1.0)):
+        rig.append(rows, dtype=dtype, theta=1e4, norm=scale == 1.0, scale=scale, q_heads=10)
+        rig.check()
+    q, q64 = rig.draw(3, 10, d, dtype=dtype)
+    check_attention(rig, [1, 1, 1], q, q64, rig.gpu.attention(rig.batch([1, 1, 1]), q, out_dtype=T().float32), F32)
+    with pytest.raises(B.GpError):
+        rig.gpu.select(rig.batch([1, 1, 1]), q, 3, 1, 1)
