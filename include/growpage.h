@@ -542,6 +542,12 @@ int gp_qcache_append(const gp_qcache* cache, const gp_qbatch* batch, const gp_qr
 /* Attention of the batch's rows over the cache: out = softmax(q.k / sqrt(d)).v over the slots that a row sees, per
  * query head, KV head g / G.  Single tokens, drafts and chunks of prompts alike.  q is in cache form (as
  * gp_qcache_append leaves it), finite.
+ * What is held in what: logits, maxima and the sum of weights in fp32; queries in fp16 after a power of two (elements below 2^-28 of the row's
+ * largest lose bits); the weights that multiply values in fp16, once for 16-bit outputs (2^-12 of a weight: an fp16 result is off by 2.9e-4
+ * where fp32 weights would leave 2.1e-4 of its own rounding; a bf16 one by no more than its own) and in two terms for fp32 ones (2^-22).  A weight
+ * below 2^-31 of the largest (times the scale of its values, for many rows) counts in the sum of weights but not in that of the values.  Sums of values are
+ * fp32, kept relative to the largest scale in them; those of many rows grow inside the tensor cores, over all steps of a stretch.
+ * A value that is no number makes its channel NaN for the rows that see it, a key that is none the whole head.
  *   q, q_stride  device [n_rows][n_q_heads][d] of `type` (GP_TYPE_BF16, GP_TYPE_F16), elements from row to row (a
  *                multiple of 8), 16-byte aligned
  *   pages        NULL: all pages.  Else device int32 [n_rows][n_kv_heads][n_list]: the pages (places in the sequence's
@@ -559,7 +565,7 @@ size_t gp_qcache_attention_bytes(const gp_qcache* cache, const gp_qbatch* batch,
 /* Test support, like gp_test_withhold: `what` names hand-overs that gp_qcache_attention then does not make (1 the kernel for few rows
  * of a sequence and lists: the first tiles of the first sequence's first head are never complete; 2 the kernel for many rows: the first keys of
  * its first thread block are never reported; 0 none), `cycles` is the time after which waits give up (0 = the default, 2^32).  The
- * thread block concerned sets bit 1 of the status word, issues nothing more and ends; the others are not affected.  Applies to the calls that
+ * thread block concerned sets 1 in the status word, issues nothing more and ends; the others are not affected.  Applies to the calls that
  * the calling thread issues after it. */
 int gp_qcache_test_withhold(int32_t what, int64_t cycles);
 

@@ -127,7 +127,7 @@ __device__ __forceinline__ void qp_wait(QpShared& sh, const QtArgs& a, uint64_t*
 }
 // Whether no wait of the block has given up; the same in all lanes.  In a block with one that has, all waits end at once: its warps that issue products leave at the next step
 // and wait for what they issued, the others go through the rest of their steps and turns with whatever lies there, and no result is written.  (Asked for behind each wait
-// of the issuing warps: chunks 218 us for 214; by the warps that convert 4 more, by those of weights 7.)
+// of the issuing warps: chunks 218 us for 214; in every step by the warps that convert 3 more, by those of weights 7.)
 __device__ __forceinline__ bool qp_alive(const QpShared& sh) { return !__any_sync(0xffffffffu, *reinterpret_cast<const volatile int*>(&sh.dead)); }
 
 // The line of work (as in the other kernel): sequence by sequence, KV head by KV head, tile of rows by tile of rows, measured in tokens.  Tile t of
@@ -248,7 +248,7 @@ struct QpWalk {
 // sum of p' times codes.  The sum of weights has a maximum of its own, m of s: L = sum of 2^(s - m), taken of p' group by group times 2^(M - m - e).  Both are whole
 // numbers, so that nothing is lost where they grow.  For that sum's sake no e counts as less than M - m - 80: a token of such a group has at most 2^-50 of the
 // largest p' then (its values count for nothing either way), and keeps a weight down to 2^-46 of the largest.  out = 2^(M - m) O / L.
-// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 195 us, 845 TFLOP/s.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 197 us, 838 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
 // d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2100 cycles for two
 // warps a scheduler; and 20 000 cycles between two units.
