@@ -532,7 +532,7 @@ typedef struct gp_qrows {
 
 /* Puts the batch's rows into the cache: normalised (optional), rotated (optional), in e4m3, with the scales and, where
  * the cache has them, the bounds of the pages they touch; the queries with them.  Keys are computed in fp64 (their
- * largest magnitude decides the scale's exponent), queries in fp32, rounded once (the sum of a query head's squares, too: heads
+ * largest magnitude decides the scale's exponent; a code is rounded by way of fp32), queries in fp32, rounded once (the sum of a query head's squares, too: heads
  * whose mean square plus eps lies outside fp32's normal numbers, 2^-126 to 2^128, are not normalised rightly).  Rows that lie in no slot
  * below max_len (or below 0) leave nothing in the cache, and their q_out as it was.  k, v, q, q_out 16-byte aligned;
  * a page that receives rows must belong to one sequence of the batch only.  Sequences by themselves may have their
@@ -543,10 +543,11 @@ int gp_qcache_append(const gp_qcache* cache, const gp_qbatch* batch, const gp_qr
  * query head, KV head g / G.  Single tokens, drafts and chunks of prompts alike.  q is in cache form (as
  * gp_qcache_append leaves it), finite.
  * What is held in what: logits, maxima and the sum of weights in fp32; queries in fp16 after a power of two (elements below 2^-28 of the row's
- * largest lose bits); the weights that multiply values in fp16, once for 16-bit outputs (2^-12 of a weight: an fp16 result is off by 2.9e-4
+ * largest lose bits); the weights that multiply values in fp16, once for 16-bit outputs (2^-11 of a weight: an fp16 result is off by 2.9e-4
  * where fp32 weights would leave 2.1e-4 of its own rounding; a bf16 one by no more than its own) and in two terms for fp32 ones (2^-22).  A weight
  * below 2^-31 of the largest (times the scale of its values, for many rows) counts in the sum of weights but not in that of the values.  Sums of values are
  * fp32, kept relative to the largest scale in them; those of many rows grow inside the tensor cores, over all steps of a stretch.
+ * Logits are expected below 2^26 (to base 2) in magnitude: beyond, fp32 does not hold what tells one from another, and results may be NaN.
  * A value that is no number makes its channel NaN for the rows that see it, a key that is none the whole head.
  *   q, q_stride  device [n_rows][n_q_heads][d] of `type` (GP_TYPE_BF16, GP_TYPE_F16), elements from row to row (a
  *                multiple of 8), 16-byte aligned

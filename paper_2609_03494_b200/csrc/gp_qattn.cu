@@ -80,10 +80,13 @@ __device__ __forceinline__ long long qt_head_granules(const QcDev& c, const QtAr
 // e4m3 codes are exact in fp16, and so are the products' factors: a query is brought to a largest magnitude of 2^14 by a power of two (what is
 // 2^-28 of the row's largest or more keeps all its bits), the scales of pages are multiplied into fp32 results: a tile of 16 tokens lies in
 // one page, so one scale for S and one for the tile's part of O.  Weights are computed in fp32 and rounded to fp16: once for 16-bit results
-// (2^-12 of a weight, an eighth of a bf16 result's own rounding), as two terms (22 bits) for fp32 ones (TERMS).  Sums of weights are fp32.
+// (2^-11 of a weight at most, an eighth of a bf16 result's own rounding), as two terms (22 bits) for fp32 ones (TERMS).  Sums of weights are fp32.
 // No sum grows over tiles inside the tensor core.
 // The maximum that weights refer to is only brought up to date when a logit passes it by 2^7: until then a tile needs no exchange between
-// lanes.  Weights times 2^8 then stay below 2^15, and fp16 reaches down to 2^-32 of the largest.
+// lanes.  Weights times 2^8 then stay below 2^15, and fp16 reaches down to 2^-32 of the largest; a token that the maximum was taken from has 2^8, so one
+// that outweighs all others loses nothing to fp16.
+// O is held times 2^-e, with 2^e the largest scale of the values of the 32 tiles that a warp looks up at a time and of those before: no sum on the way passes what
+// fp32 holds (weights of 2^15 times values of 448 * 2^119 would), and a tile's own factor is at most 1.
 // Keys: ldmatrix gives a lane four consecutive codes of a token, which are its elements of both halves of a k step when the queries are
 // read in the same order.  Values: ldmatrix.trans moves pairs of codes, i.e. two channels of two tokens in a register; a byte permutation
 // puts them in pairs of tokens, and the two channels go to rows r and r + 8 of the product.
@@ -433,7 +436,7 @@ qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs 
           float corr[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float mn = fmaxf(m[n][e], ceilf(mx[e]) - QT_LIFT);
+            const float mn = fmaxf(m[n][e], mx[e] - QT_LIFT);
             corr[e] = m[n][e] == mn ? 1.f : qt_exp2(m[n][e] - mn);
             m[n][e] = mn;
           }

@@ -15,7 +15,7 @@ constexpr float QT_NONE = -3.3e38f;            // a maximum of nothing
 
 // A part of a column's result: D sums of weighted values, m, the sum of weights l, e (and a word that nobody reads).  With logits s to base 2, weights are 2^(s - m) and the
 // values' sums are held times 2^-e, so that no sum on the way passes what fp32 holds where the result does not: what is meant is 2^m l and 2^(m + e) o.
-// m and e are whole numbers in the kernels: what is rescaled loses no bits.
+// e is a whole number.
 __host__ __device__ constexpr int qt_part(int d) { return d + 4; }
 
 struct QtArgs {

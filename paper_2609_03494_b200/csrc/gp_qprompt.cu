@@ -245,9 +245,10 @@ struct QpWalk {
 // rows behind) are set at the end.
 // Scales of pages cost nothing per element: 16 columns of S lie in one page, so the keys' scale joins the factor of the logits s and the exponent e of
 // the values' scale the constant that is added before the exponential: p' = 2^(s + e - M), M the running maximum of s + e of the tokens that the row sees.  O is then a plain
-// sum of p' times codes.  The sum of weights has a maximum of its own, m of s: L = sum of 2^(s - m), taken of p' group by group times 2^(M - m - e).  Both are whole
-// numbers, so that nothing is lost where they grow.  For that sum's sake no e counts as less than M - m - 80: a token of such a group has at most 2^-50 of the
-// largest p' then (its values count for nothing either way), and keeps a weight down to 2^-46 of the largest.  out = 2^(M - m) O / L.
+// sum of p' times codes.  The sum of weights has a maximum of its own, m of s: L = sum of 2^(s - m), taken of p' group by group times 2^(M - m - e).  M - m is a whole
+// number (`apart`), so that O and L refer to each other exactly; M itself is not, and the largest p' is 2^8 when M is its own.  For L's sake no e counts as less than
+// M - m - 80: a token of such a group has at most 2^-50 of the largest p' then (its values count for nothing either way), and keeps a weight down to 2^-46 of the
+// largest.  out = 2^(M - m) O / L.
 // Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 197 us, 838 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
 // d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2100 cycles for two
@@ -513,7 +514,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       }
       __syncwarp();
       if (lane == 0 && p.n_steps > 0) qp_arrive(&sh.q_full[half]);
-      float M = -INFINITY, m = -INFINITY, L = 0.f;      // M: less the lift
+      float M = -INFINITY, apart = 0.f, L = 0.f;        // M: less the lift; M - m
       for (int j = 0; j < p.n_steps; ++j) {
         const int s = n + j;
         const int slot = s & (2 * QP_RING - 1);
@@ -561,14 +562,14 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
             const float t = fmaxf(m0, m1) * f[g];
             ms = fmaxf(ms, t); mx = fmaxf(mx, t + ev[g]);
           }
-          const bool over = mx > M + (QP_LIFT + QP_SLACK) || ms > m + QP_LAG;
+          const bool over = mx > M + (QP_LIFT + QP_SLACK) || ms > M - apart + QP_LAG;
           if (__any_sync(0xffffffffu, over)) {
             float corr = 1.f;
             if (over) {
-              const float to = fmaxf(M, ceilf(mx) - QP_LIFT), top = fmaxf(m, ceilf(ms));      // (minus infinity at first)
-              corr = qt_exp2(M - to);
-              L *= qt_exp2(m - top);
-              M = to; m = top;
+              const float to = fmaxf(M, mx - QP_LIFT), by = M - to, now = ceilf(to - fmaxf(M - apart, ms));      // (minus infinity at first; m may fall by less than 1)
+              corr = qt_exp2(by);
+              L *= qt_exp2(by + (now - apart));
+              M = to; apart = now;
             }
             if (j > 0 && __any_sync(0xffffffffu, corr != 1.f)) {
               qp_wait(sh, a, &sh.o_full[half][(s - 1) & (QP_RING - 1)], ((s - 1) / QP_RING) & 1);      // all of O is there
@@ -584,7 +585,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
               }
             }
           }
-          const float zero = M == -INFINITY ? 0.f : M, apart = M == -INFINITY ? 0.f : M - m;
+          const float zero = M == -INFINITY ? 0.f : M;
 #pragma unroll
           for (int g = 0; g < 4; ++g) ev[g] = fmaxf(ev[g], apart - QP_FAR);
           qp_turn(turn + half);
@@ -639,7 +640,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
       auto place = [&](int col, int pc) { return stage + (pc >> 3) * QP_QBLOCK + col * 128 + (((pc & 7) ^ (col & 7)) << 4); };
       constexpr int PIECES = D / 8;                     // of 16 bytes, of a column there
       const bool wide = parts || a.out_type == GP_TYPE_F32;      // two rounds of half of the channels in 32 bits, else one of all in 16
-      const float apart = M == -INFINITY ? 0.f : M - m, inv = parts ? 1.f : L != 0.f ? 1.f / L : 0.f, scale = parts ? 1.f : exp2f(apart);      // (a NaN sum is not 0)
+      const float inv = parts ? 1.f : L != 0.f ? 1.f / L : 0.f, scale = parts ? 1.f : exp2f(apart);      // (a NaN sum is not 0)
 #pragma unroll 1
       for (int round = 0; round < (wide ? 2 : 1); ++round) {
         const int chans = wide ? D / 2 : D;
@@ -702,7 +703,7 @@ qp_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a) {
         }
         __syncwarp();
       }
-      if (parts && real) *reinterpret_cast<float4*>(parts + (size_t)t128 * ST + D) = make_float4(fmaxf(m, QT_NONE), L, apart, 0.f);
+      if (parts && real) *reinterpret_cast<float4*>(parts + (size_t)t128 * ST + D) = make_float4(fmaxf(M - apart, QT_NONE), L, apart, 0.f);
     }
     if (!half) qp_turn(turn);
   }
