@@ -93,9 +93,9 @@ __device__ __forceinline__ long long qt_head_granules(const QcDev& c, const QtAr
 // Values that are no numbers: a weight of 0 would carry them to rows that do not see them.  Where the rows of a tile see different tokens, the codes of tokens that
 // not all of them see are looked at in shared memory; a NaN counts as 0 there, and at the end the least row that sees one is found per channel.
 // A warp brings its own tiles in, two at a time by TMA, into its own stages: nothing in the loop waits for another warp.
-// What bounds it (with the join): memory where sequences are long (three of 60 001 to 131 071 tokens, 8 KV heads, groups of 8, d = 128: 124 us, 5.7 TB/s); where
-// they are short, the start and end of a block's units (64 of 60 to 4000 tokens, groups of 4: 53 us, 5.0 TB/s); with many columns, instructions (five rows of 48
-// sequences, 20 columns, d = 64: 71 us for 146 MB).
+// What bounds it (with the join): memory where sequences are long (three of 60 001 to 131 071 tokens, 8 KV heads, groups of 8, d = 128: 123 us, 5.8 TB/s); where
+// they are short, the start and end of a block's units (64 of 60 to 4000 tokens, groups of 4: 52 us, 5.1 TB/s); with many columns, instructions (five rows of 48
+// sequences, 20 columns, d = 64: 70 us for 146 MB).
 template <int D, int NT, int TERMS, bool LIST>
 __global__ void __launch_bounds__(QT_THREADS, qt_resident(NT, D))
 qt_split_kernel(const __grid_constant__ QcDev c, const __grid_constant__ QtArgs a, const __grid_constant__ CUtensorMap map) {

@@ -249,7 +249,7 @@ struct QpWalk {
 // number (`apart`), so that O and L refer to each other exactly; M itself is not, and the largest p' is 2^8 when M is its own.  For L's sake no e counts as less than
 // M - m - 80: a token of such a group has at most 2^-50 of the largest p' then (its values count for nothing either way), and keeps a weight down to 2^-46 of the
 // largest.  out = 2^(M - m) O / L.
-// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 197 us, 838 TFLOP/s.
+// Measured: 301 to 1101 rows of three sequences of up to 9000 tokens, 8 KV heads, groups of 4, d = 128 (165 GFLOP): 196 us, 842 TFLOP/s.
 // What would bound it: 2 x 128 x 64 exponentials a step and SM (16 a cycle) against 2 x 128 x 64 x 2 d multiply-adds (4096 a cycle): with
 // d = 128 the same, 1024 cycles.  What does: the chain of a warp's step (logits, their largest, exponentials, handing on), 2100 cycles for two
 // warps a scheduler; and 20 000 cycles between two units.
